@@ -359,6 +359,78 @@ int32_t sf_encoder_forward_fp8(const sf_desc *desc, const sf_compact_layer *laye
                                uint8_t *oq_out, void *workspace, size_t workspace_bytes,
                                void *stream);
 
+/* ------------------------------------------------------------------------
+ * Products in 8-bit integers with a scale for each token and each output
+ * feature (the integer counterpart of the FP8 arithmetic above, whose scales
+ * are one per tensor and fixed offline).  Codes are signed, symmetric:
+ *     Q(x): a = max_j |x_j| of a row, code_j = 127 x_j / a rounded to the nearest
+ *           integer (ties to even, decided exactly), scale = a / 127 (fp32);
+ *           a = 0: codes and scale 0; a row with an infinity or NaN: codes 0 and
+ *           scale NaN, so that every product with that row, and no other, is NaN.
+ * Sums of code products are exact (int32).
+ *
+ * sf_quantize_i8_rows: codes [rows, n] (row stride ldc bytes) and scale [rows]
+ * of x [rows, n] (dtype SF_F32 or this build's 16-bit type, row stride ldx
+ * elements).  Any n, stride and alignment; whole 16-byte accesses where x and
+ * its rows lie on 16 bytes, codes and its rows on 8 and n % 8 == 0.  It is also how
+ * weights are quantised offline: a row of W [N, K] is an output feature.
+ *
+ * sf_linear_i8_forward: Y = act(Q(X) W^T s + bias) (+ R), the rows of X
+ * quantised as they come.  X [rows, K], R and Y [rows, N] of type dtype with
+ * strides ldx, ldr, ldy in elements; R may be NULL and may be Y.  sf_linear_i8: W
+ * codes [N, K] (16-byte aligned, stride ldw a multiple of 16), s [N] fp32, bias
+ * [N] of type dtype or NULL.  act: SF_ACT_NONE, SF_RELU, SF_GELU_ERF.  K a
+ * multiple of 16, at most 65536.  Otherwise rounded once, to dtype.
+ *
+ * sf_pruned_ffn_i8_forward: the pruned FFN with both products in integers,
+ *     h = act(Q(LN2(x)) W1q s1 + b1)                      (fp32)
+ *     y = Q(h) W2q s2 + b2 (+ x)                          -> 16 bits
+ * X, Y [B*L, d], 16 bits (Y may not alias X), pattern_id as in
+ * sf_pruned_ffn_forward; pre_ln = 0 quantises X itself.  d a multiple of 16, at
+ * most 4096, d_ff <= 65472.  sf_ffn_i8, for all P patterns with Fp =
+ * sf_ffn_padded(k_ffn):
+ *   W1q [P, Fp, d]  codes of the kept channels (ascending), zero above F'
+ *   s1  [P, Fp]     their scales, zero above F'
+ *   b1  [P, Fp]     16 bits, zero above F'; NULL iff the dense b1 is
+ *   W2Tq [P, d, Fp] W2Tq[n, j] = W2[ffn_idx[j], n], zero above F'
+ *   s2  [d]         scale of output feature n;  b2, ln2_g, ln2_b [d]: the dense arrays
+ * sf_compact_ffn_i8 fills W1q, s1, b1, W2Tq from a dense int8 layer (W1, W2
+ * [d_ff, d] codes, s1 [d_ff], s2 [d] - one scale per column of W2 -, b1 [d_ff] or
+ * NULL) and this layer's slice of ffn_idx (bit-exact data movement).
+ */
+enum { SF_ACT_NONE = -1 };
+int32_t sf_quantize_i8_rows(const void *x, int32_t dtype, int64_t rows, int32_t n, int64_t ldx,
+                            int8_t *codes, int64_t ldc, float *scale, void *stream);
+typedef struct sf_linear_i8 {
+    int32_t N, K;
+    const void *W; int64_t ldw;
+    const float *s;
+    const void *bias;
+} sf_linear_i8;
+size_t sf_linear_i8_workspace_bytes(int64_t rows, int32_t K);
+int32_t sf_linear_i8_forward(const sf_linear_i8 *linear_host, int32_t dtype, int64_t rows,
+                             const void *X, int64_t ldx, int32_t act, const void *R, int64_t ldr,
+                             void *Y, int64_t ldy, void *workspace, size_t workspace_bytes,
+                             void *stream);
+typedef struct sf_dense_ffn_i8 {
+    const int8_t *W1, *W2;
+    const float *s1;
+    const void *b1;
+} sf_dense_ffn_i8;
+typedef struct sf_ffn_i8 {
+    int32_t k_ffn;             /* F' */
+    int32_t reserved;
+    int8_t *W1q; float *s1; void *b1;
+    int8_t *W2Tq; const float *s2;
+    const void *b2, *ln2_g, *ln2_b;
+} sf_ffn_i8;
+int32_t sf_compact_ffn_i8(const sf_desc *desc, int32_t layer, const sf_dense_ffn_i8 *dense_host,
+                          const int32_t *ffn_idx, const sf_ffn_i8 *ffn_host, void *stream);
+size_t sf_pruned_ffn_i8_workspace_bytes(const sf_desc *desc, int32_t k_ffn);
+int32_t sf_pruned_ffn_i8_forward(const sf_desc *desc, const sf_ffn_i8 *ffn_host, const void *X,
+                                 const int32_t *pattern_id, int32_t pre_ln, int32_t add_residual,
+                                 void *Y, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Element strides of a [B, heads, L, dh] tensor whose last dimension is
  * contiguous (for V with v_transposed: a [B, groups, dh, L] tensor whose L
  * dimension is contiguous and `l` is the stride between dh rows). */

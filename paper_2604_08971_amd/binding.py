@@ -22,7 +22,7 @@ _libs = {}
 _half = "bf16"
 
 SF_F32, SF_BF16, SF_F16 = 0, 1, 2
-SF_RELU, SF_GELU_ERF = 0, 1
+SF_RELU, SF_GELU_ERF, SF_ACT_NONE = 0, 1, -1
 SF_FLAG_FINAL_LN = 1
 
 EXPORTS = ["sf_last_error", "sf_num_active", "sf_ffn_padded", "sf_gate_scores_to_masks",
@@ -38,7 +38,8 @@ EXPORTS = ["sf_last_error", "sf_num_active", "sf_ffn_padded", "sf_gate_scores_to
            "sf_sparse_gqa_static_capacity", "sf_sparse_gqa_forward_static", "sf_ceiling_mfma_launch",
            "sf_ceiling_copy_launch", "sf_token_pack_rows_max", "sf_token_pack", "sf_token_unpack",
            "sf_encoder_packed_workspace_bytes", "sf_encoder_forward_packed", "sf_sparse_gqa_plan",
-           "sf_gemm_kernel"]
+           "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_workspace_bytes", "sf_linear_i8_forward",
+           "sf_compact_ffn_i8", "sf_pruned_ffn_i8_workspace_bytes", "sf_pruned_ffn_i8_forward"]
 SF_GATE_RELU, SF_GATE_TANH = 0, 1
 SF_KERNEL_GEMM, SF_KERNEL_SCORE, SF_KERNEL_ATTEND, SF_KERNEL_ATTENTION, SF_KERNEL_LAYERNORM = 0, 1, 2, 3, 4
 
@@ -89,6 +90,20 @@ class SfProjFp8(C.Structure):
                 + [(n, C.c_float) for n in ("s_qkv", "so", "sx1", "sa")])
 
 
+class SfLinearI8(C.Structure):
+    _fields_ = [("N", C.c_int32), ("K", C.c_int32), ("W", C.c_void_p), ("ldw", C.c_int64), ("s", C.c_void_p),
+                ("bias", C.c_void_p)]
+
+
+class SfDenseFfnI8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("W1", "W2", "s1", "b1")]
+
+
+class SfFfnI8(C.Structure):
+    _fields_ = ([("k_ffn", C.c_int32), ("reserved", C.c_int32)]
+                + [(n, C.c_void_p) for n in ("W1q", "s1", "b1", "W2Tq", "s2", "b2", "ln2_g", "ln2_b")])
+
+
 class SfTokenPackPlan(C.Structure):
     _fields_ = ([("Tc", C.c_int32)]
                 + [(n, C.c_void_p) for n in ("len", "u_active", "row0", "ext", "valid_c", "blk_pattern", "src_row",
@@ -135,7 +150,8 @@ def lib():
         L.sf_last_error.restype = C.c_char_p
         for n in ("sf_sparse_gqa_workspace_bytes", "sf_pruned_ffn_workspace_bytes", "sf_encoder_workspace_bytes",
                   "sf_moe_ffn_workspace_bytes", "sf_pruned_ffn_fp8_workspace_bytes", "sf_encoder_fp8_workspace_bytes",
-                  "sf_sparse_gqa_static_capacity", "sf_encoder_packed_workspace_bytes"):
+                  "sf_sparse_gqa_static_capacity", "sf_encoder_packed_workspace_bytes", "sf_linear_i8_workspace_bytes",
+                  "sf_pruned_ffn_i8_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         for n in ("sf_num_active", "sf_ffn_padded", "sf_gate_scores_to_masks", "sf_compact_heads_channels",
                   "sf_sparse_gqa_forward", "sf_pruned_ffn_forward", "sf_encoder_forward", "sf_profile_begin",
@@ -146,7 +162,7 @@ def lib():
                   "sf_active_projection_rows", "sf_compact_proj_fp8", "sf_encoder_forward_fp8", "sf_proj_fp8_padded",
                   "sf_presence_to_key_valid", "sf_sparse_gqa_forward_static", "sf_token_pack_rows_max",
                   "sf_token_pack", "sf_token_unpack", "sf_encoder_forward_packed", "sf_sparse_gqa_plan",
-                  "sf_gemm_kernel"):
+                  "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_forward", "sf_compact_ffn_i8", "sf_pruned_ffn_i8_forward"):
             getattr(L, n).restype = C.c_int32
         L.sf_gemm_kernel.argtypes = [C.POINTER(SfDesc)] + [C.c_int32] * 4
         L.sf_sparse_gqa_plan.argtypes = [C.POINTER(SfDesc), C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
@@ -218,6 +234,16 @@ def lib():
         L.sf_budget_search.argtypes = [C.POINTER(SfDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.c_void_p, C.c_void_p]
+        L.sf_quantize_i8_rows.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int64,
+                                          C.c_void_p, C.c_void_p]
+        L.sf_linear_i8_workspace_bytes.argtypes = [C.c_int64, C.c_int32]
+        L.sf_linear_i8_forward.argtypes = [C.POINTER(SfLinearI8), C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_int32,
+                                           C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sf_compact_ffn_i8.argtypes = [C.POINTER(SfDesc), C.c_int32, C.POINTER(SfDenseFfnI8), C.c_void_p,
+                                        C.POINTER(SfFfnI8), C.c_void_p]
+        L.sf_pruned_ffn_i8_workspace_bytes.argtypes = [C.POINTER(SfDesc), C.c_int32]
+        L.sf_pruned_ffn_i8_forward.argtypes = [C.POINTER(SfDesc), C.POINTER(SfFfnI8), C.c_void_p, C.c_void_p, C.c_int32,
+                                               C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.sf_profile_begin.argtypes = [C.c_int32, C.c_int32]
         L.sf_profile_end.argtypes = [C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.sf_num_active.argtypes = [C.POINTER(SfDesc)]
@@ -238,6 +264,13 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    """The current stream, for a call on t's device: that has to be the current device, where the launches go."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise SentryFuseError(f"tensors on {t.device}, which is not the current device")
+    return torch.cuda.current_stream().cuda_stream
 
 
 def torch_dtype(dtype: int):
@@ -652,6 +685,151 @@ def pruned_ffn_fp8_forward(desc: SfDesc, ffn: CompactFfnFp8, X: torch.Tensor,
                                          _stream())
     _check(rc, "sf_pruned_ffn_fp8_forward")
     return (Y, xq, hq) if want_codes else Y
+
+
+# ---------------------------------------------------------- products in 8-bit integers
+_SF_OF = {torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16}
+
+
+def _rows_of(x: torch.Tensor, what: str):
+    """(rows, row stride) of a tensor whose leading dimensions are one run of equally spaced rows."""
+    assert x.dim() >= 1 and (x.shape[-1] <= 1 or x.stride(-1) == 1), f"{what}: the last dimension has to be contiguous"
+    if x.dim() <= 2:
+        return (x.shape[0], x.stride(0)) if x.dim() == 2 else (1, x.shape[-1])
+    assert x.is_contiguous(), f"{what}: more than two dimensions have to be contiguous"
+    return x.numel() // max(x.shape[-1], 1), x.shape[-1]
+
+
+def quantize_i8_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """int8 codes of x and one scale per row (fp32): x ~ codes * scale.  x [rows, n] with any row stride, or contiguous of
+    more dimensions.  Returns (codes, scale)."""
+    rows, ldx = _rows_of(x, "x")
+    n = x.shape[-1]
+    if codes is None:
+        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    crows, ldc = _rows_of(codes, "codes")
+    assert codes.dtype == torch.int8 and codes.shape[-1] == n and crows == rows
+    assert scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == rows
+    _check(lib().sf_quantize_i8_rows(x.data_ptr(), _SF_OF[x.dtype], rows, n, max(ldx, n), codes.data_ptr(), max(ldc, n), scale.data_ptr(),
+                                     _stream_of(x)), "sf_quantize_i8_rows")
+    return codes, scale
+
+
+class LinearI8:
+    """A projection's weights: codes [N, K] int8 (rows may be strided), a scale per output feature, an optional bias."""
+
+    def __init__(self, codes: torch.Tensor, scale: torch.Tensor, bias: Optional[torch.Tensor] = None):
+        assert codes.dtype == torch.int8 and codes.dim() == 2 and codes.stride(1) == 1
+        self.N, self.K = codes.shape
+        assert scale.dtype == torch.float32 and scale.is_contiguous() and tuple(scale.shape) == (self.N,)
+        assert bias is None or (bias.is_contiguous() and tuple(bias.shape) == (self.N,))
+        self.codes, self.scale, self.bias = codes, scale, bias
+        self.struct = SfLinearI8(self.N, self.K, codes.data_ptr(), codes.stride(0), scale.data_ptr(),
+                                 None if bias is None else bias.data_ptr())
+        self.ref = C.byref(self.struct)
+
+    @classmethod
+    def quantize(cls, W: torch.Tensor, bias: Optional[torch.Tensor] = None) -> "LinearI8":
+        """From W [N, K] in fp32 or 16 bits (K a multiple of 16)."""
+        codes, scale = quantize_i8_rows(W.contiguous())
+        return cls(codes, scale, bias)
+
+
+def linear_i8_workspace_bytes(rows: int, K: int) -> int:
+    return int(lib().sf_linear_i8_workspace_bytes(int(rows), int(K)))
+
+
+def linear_i8_forward(lin: LinearI8, X: torch.Tensor, act: int = SF_ACT_NONE, residual: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """X [..., K] in fp32 or this build's 16-bit type -> [..., N]; rows are quantised as they come."""
+    rows, ldx = _rows_of(X, "X")
+    N, K, dt = lin.N, lin.K, X.dtype
+    assert X.shape[-1] == K and (lin.bias is None or lin.bias.dtype == dt)
+    if out is None:
+        out = torch.empty(X.shape[:-1] + (N,), dtype=dt, device=X.device)
+    orows, ldy = _rows_of(out, "out")
+    assert out.dtype == dt and out.shape[-1] == N and orows == rows
+    r, ldr = None, N
+    if residual is not None:
+        rrows, ldr = _rows_of(residual, "residual")
+        assert residual.dtype == dt and residual.shape[-1] == N and rrows == rows
+        r = residual.data_ptr()
+    if ws is None:
+        ws = workspace(linear_i8_workspace_bytes(max(rows, 1), K), X.device)
+    _check(lib().sf_linear_i8_forward(lin.ref, _SF_OF[dt], rows, X.data_ptr(), max(ldx, K), act, r, max(ldr, N), out.data_ptr(), max(ldy, N),
+                                      ws.data_ptr(), ws.numel(), _stream_of(X)), "sf_linear_i8_forward")
+    return out
+
+
+class CompactFfnI8:
+    """FFN weights of one layer as int8 codes with a scale per channel, compacted for all patterns.  Buffers that are not
+    given are allocated (to be filled by compact_ffn_i8)."""
+
+    def __init__(self, desc: SfDesc, k_ffn: int, W1q: Optional[torch.Tensor] = None, s1: Optional[torch.Tensor] = None,
+                 W2Tq: Optional[torch.Tensor] = None, s2: Optional[torch.Tensor] = None, b1: Optional[torch.Tensor] = None,
+                 b2: Optional[torch.Tensor] = None, ln2_g: Optional[torch.Tensor] = None,
+                 ln2_b: Optional[torch.Tensor] = None, with_b1: bool = False, device="cuda"):
+        P, d = desc.P, desc.d_model
+        self.k_ffn = int(k_ffn)
+        Fp = self.Fp = ffn_padded(desc, self.k_ffn)
+        new = lambda t, shape, dt: torch.empty(shape, dtype=dt, device=device) if t is None else t
+        self.W1q, self.s1 = new(W1q, (P, Fp, d), torch.int8), new(s1, (P, Fp), torch.float32)
+        self.W2Tq = new(W2Tq, (P, d, Fp), torch.int8)
+        self.b1 = new(b1, (P, Fp), torch_dtype(desc.dtype)) if with_b1 or b1 is not None else None
+        self.s2, self.b2, self.ln2_g, self.ln2_b = s2, b2, ln2_g, ln2_b
+        for t, shape, dt in ((self.W1q, (P, Fp, d), torch.int8), (self.s1, (P, Fp), torch.float32), (self.W2Tq, (P, d, Fp), torch.int8),
+                             (self.b1, (P, Fp), torch_dtype(desc.dtype)), (s2, (d,), torch.float32),
+                             (b2, (d,), torch_dtype(desc.dtype)), (ln2_g, (d,), torch_dtype(desc.dtype)), (ln2_b, (d,), torch_dtype(desc.dtype))):
+            assert t is None or (t.dtype == dt and t.is_contiguous() and tuple(t.shape) == shape), (tuple(t.shape), shape)
+        self.struct = SfFfnI8(self.k_ffn, 0, *[None if t is None else t.data_ptr()
+                                               for t in (self.W1q, self.s1, self.b1, self.W2Tq, s2, b2, ln2_g, ln2_b)])
+        self.ref = C.byref(self.struct)
+
+
+def quantize_ffn_i8(dense: Dict[str, torch.Tensor]) -> Dict[str, torch.Tensor]:
+    """Dense FFN weights (W1, W2 [d_ff, d], unit-major) -> W1, W2 int8 with s1 [d_ff] (a scale per channel of W1) and s2 [d]
+    (one per output feature, a column of W2); everything else is handed on."""
+    W1, s1 = quantize_i8_rows(dense["W1"])
+    W2t, s2 = quantize_i8_rows(dense["W2"].t().contiguous())
+    return dict(dense, W1=W1, s1=s1, W2=W2t.t().contiguous(), s2=s2)
+
+
+def compact_ffn_i8(desc: SfDesc, layer: int, dense8: Dict[str, torch.Tensor], masks: Dict[str, torch.Tensor],
+                   k_ffn: int, out: Optional[CompactFfnI8] = None) -> CompactFfnI8:
+    """dense8: what quantize_ffn_i8 returns (W1, W2 int8, s1, s2, and b1, b2, ln2_g, ln2_b in the model dtype)."""
+    F, d = desc.d_ff, desc.d_model
+    for n, shape, dt in (("W1", (F, d), torch.int8), ("W2", (F, d), torch.int8), ("s1", (F,), torch.float32), ("s2", (d,), torch.float32)):
+        assert dense8[n].dtype == dt and dense8[n].is_contiguous() and tuple(dense8[n].shape) == shape, n
+    b1 = dense8.get("b1")
+    assert b1 is None or (b1.dtype == torch_dtype(desc.dtype) and b1.is_contiguous() and tuple(b1.shape) == (F,)), "b1"
+    cf = out if out is not None else CompactFfnI8(desc, k_ffn, s2=dense8["s2"], b2=dense8.get("b2"), ln2_g=dense8.get("ln2_g"),
+                                                  ln2_b=dense8.get("ln2_b"), with_b1=b1 is not None, device=dense8["W1"].device)
+    assert cf.k_ffn == int(k_ffn)
+    ds = SfDenseFfnI8(*[_ptr(t) for t in (dense8["W1"], dense8["W2"], dense8["s1"], b1)])
+    _check(lib().sf_compact_ffn_i8(C.byref(desc), int(layer), C.byref(ds), _ptr(masks["ffn_idx"]), cf.ref, _stream()), "sf_compact_ffn_i8")
+    return cf
+
+
+def pruned_ffn_i8_workspace_bytes(desc: SfDesc, k_ffn: int) -> int:
+    return int(lib().sf_pruned_ffn_i8_workspace_bytes(C.byref(desc), int(k_ffn)))
+
+
+def pruned_ffn_i8_forward(desc: SfDesc, ffn: CompactFfnI8, X: torch.Tensor, pattern_id: Optional[torch.Tensor] = None,
+                          pre_ln: bool = True, add_residual: bool = True, out: Optional[torch.Tensor] = None,
+                          ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """X [B, L, d] (or [B*L, d]) in 16 bits, contiguous -> Y."""
+    assert X.is_contiguous() and X.dtype == torch_dtype(desc.dtype) and X.numel() == desc.B * desc.L * desc.d_model
+    assert pattern_id is None or (pattern_id.dtype == torch.int32 and pattern_id.is_contiguous() and pattern_id.numel() == desc.B)
+    Y = torch.empty_like(X) if out is None else out
+    assert Y.is_contiguous() and Y.dtype == X.dtype and Y.numel() == X.numel()
+    if ws is None:
+        ws = workspace(pruned_ffn_i8_workspace_bytes(desc, ffn.k_ffn), X.device)
+    _check(lib().sf_pruned_ffn_i8_forward(C.byref(desc), ffn.ref, X.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
+                                          pre_ln, add_residual, Y.data_ptr(), ws.data_ptr(), ws.numel(),
+                                          _stream_of(X)), "sf_pruned_ffn_i8_forward")
+    return Y
 
 
 # ---------------------------------------------------------- Sparse-MoE FFN with pruned experts

@@ -654,6 +654,39 @@ extern "C" int32_t sf_compact_ffn_fp8(const sf_desc *desc, int32_t layer, const 
     return check_launch("compact_ffn_fp8");
 }
 
+// The FFN of one layer from int8-stored weights: the same gathers on bytes, and the scales and biases of the kept channels
+extern "C" int32_t sf_compact_ffn_i8(const sf_desc *desc, int32_t layer, const sf_dense_ffn_i8 *dense, const int32_t *ffn_idx,
+                                     const sf_ffn_i8 *f, void *stream)
+{
+    Dims D;
+    if (int32_t rc = read_desc(desc, D)) return rc;
+    if (!dense || !f || !ffn_idx) return fail(SF_ERR_INVALID_ARG, "compact_ffn_i8: NULL argument");
+    if (layer < 0 || layer >= D.nl) return fail(SF_ERR_INVALID_ARG, "compact_ffn_i8: layer %d out of range", layer);
+    if (D.dtype != SF_BF16) return fail(SF_ERR_UNSUPPORTED, "compact_ffn_i8: the integer path takes 16-bit activations, not fp32");
+    if (D.d % 16 || D.d > 4096 || D.F > 65472)
+        return fail(SF_ERR_SHAPE, "compact_ffn_i8: d_model a multiple of 16 up to 4096, d_ff <= 65472 required");
+    if (f->k_ffn < 1 || f->k_ffn > D.F) return fail(SF_ERR_INVALID_ARG, "compact_ffn_i8: k_ffn out of range");
+    if (!dense->W1 || !dense->s1 || !dense->W2 || !f->W1q || !f->s1 || !f->W2Tq) return fail(SF_ERR_INVALID_ARG, "compact_ffn_i8: NULL weight pointer");
+    if (dense->b1 && !f->b1) return fail(SF_ERR_INVALID_ARG, "compact_ffn_i8: compact bias buffer missing");
+    if (((uintptr_t)dense->W1 | (uintptr_t)f->W1q) & 15) return fail(SF_ERR_INVALID_ARG, "compact_ffn_i8: 16-byte aligned W1 required");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int P = D.P, d = D.d, kf = f->k_ffn, Fp = (int)align_up((size_t)kf, D.ffn_pad);
+    const int32_t *fi = ffn_idx + (size_t)layer * P * D.F;
+    auto gather = [&](const void *src, void *dst, size_t bytes) {
+        GatherRegions g{};
+        GatherRegion &r = g.r[g.n++];
+        r.src = src; r.dst = dst; r.idx = fi; r.n_dev = nullptr;
+        r.idx_stride = D.F; r.block = 1; r.n_static = kf; r.rows = Fp; r.dst_pstride = (size_t)Fp;
+        gather_rows(st, g, bytes, P);
+    };
+    gather(dense->W1, f->W1q, (size_t)d);
+    gather(dense->s1, f->s1, sizeof(float));
+    if (dense->b1) gather(dense->b1, f->b1, elem_size(D.dtype));
+    hipLaunchKernelGGL(gather_transpose_kernel<uint8_t>, dim3(ceil_div(Fp, 32), ceil_div(d, 32), P), dim3(256), 0, st, (const uint8_t *)dense->W2,
+                       (uint8_t *)f->W2Tq, fi, D.F, 1, kf, Fp, d, (size_t)d * Fp);
+    return check_launch("compact_ffn_i8");
+}
+
 // Attention projection weights kept as E4M3 codes for the FP8 arithmetic path: Wqkv8 [P, (k_head + 2 Hk) dh, d]
 // (kept Q heads, then the K and the V rows of the used groups, zero rows for unused group slots) and
 // WoT8 [P, d, Kp] with Kp = k_head dh rounded up to 128 (zero columns: the FP8 GEMM contracts over multiples of 128),
