@@ -516,6 +516,33 @@ int32_t sf_sparse_gqa_forward_static(const sf_desc *desc, int32_t nH, int32_t nG
                                      void *stream);
 
 /* ------------------------------------------------------------------------
+ * cross_gqa_forward -- cross-modal attention (Sec. 4.1: per-modality encoders
+ * followed by cross-modal attention): the L = desc->L query tokens of a sample over
+ * the Lk states of another sequence, nG K/V groups shared by nH heads,
+ *     o_i = sum_j softmax_j(q_i.k_j / sqrt(dh)) v_j   over the allowed keys j.
+ * uses desc->B, L (queries per sample), dh, dtype.
+ *   Q [B,nH,L,dh], K, V [B,nG,Lk,dh] strided (sf_strides, last dimension
+ *                contiguous, strides not negative, that of a token at most 2^22;
+ *                16 bits: multiples of 8 and tensors on 16 bytes)
+ *   head_group   [n_maps, nH] int32, head -> group; a head outside 0..nG-1 is not
+ *                computed and its columns of O stay as they were
+ *   pattern_id   [B] int32 row of head_group used by sample b, or NULL (row 0)
+ *   key_valid    [B,Lk] u8, non-zero = allowed, or NULL (all).  What a key that is
+ *                not allowed holds is never used, infinities and NaN included.  A
+ *                sample with no allowed key gets zero rows.
+ *   O            [B,L,nH*dh], row stride ldo elements; may not alias an input
+ * At most 64 heads and groups; dh 32, 64, 128 (16 bits) or a multiple of 8 up to
+ * 128 (fp32).  16-bit models: weights are rounded to 16 bits for the matrix cores
+ * and normalised by the sum of the rounded ones; everything else is fp32.
+ */
+size_t sf_cross_gqa_workspace_bytes(const sf_desc *desc, int32_t Lk, int32_t nH, int32_t nG);
+int32_t sf_cross_gqa_forward(const sf_desc *desc, int32_t nH, int32_t nG, int32_t Lk,
+                             const void *Q, sf_strides sq, const void *K, sf_strides sk,
+                             const void *V, sf_strides sv, const int32_t *head_group,
+                             const int32_t *pattern_id, const uint8_t *key_valid, void *O,
+                             int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * pruned_ffn_forward -- Sec. 4.5: Y = [X +] act(X' W1'^T + b1') W2' + b2 with
  * X' = LayerNorm(X) when pre_ln != 0, else X.  X, Y [B*L, d]; sample b uses
  * pattern pattern_id[b] (NULL: 0).  Uses k_ffn, W1, b1, W2T, b2, ln2_g, ln2_b

@@ -39,7 +39,8 @@ EXPORTS = ["sf_last_error", "sf_num_active", "sf_ffn_padded", "sf_gate_scores_to
            "sf_ceiling_copy_launch", "sf_token_pack_rows_max", "sf_token_pack", "sf_token_unpack",
            "sf_encoder_packed_workspace_bytes", "sf_encoder_forward_packed", "sf_sparse_gqa_plan",
            "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_workspace_bytes", "sf_linear_i8_forward",
-           "sf_compact_ffn_i8", "sf_pruned_ffn_i8_workspace_bytes", "sf_pruned_ffn_i8_forward"]
+           "sf_compact_ffn_i8", "sf_pruned_ffn_i8_workspace_bytes", "sf_pruned_ffn_i8_forward",
+           "sf_cross_gqa_workspace_bytes", "sf_cross_gqa_forward"]
 SF_GATE_RELU, SF_GATE_TANH = 0, 1
 SF_KERNEL_GEMM, SF_KERNEL_SCORE, SF_KERNEL_ATTEND, SF_KERNEL_ATTENTION, SF_KERNEL_LAYERNORM = 0, 1, 2, 3, 4
 
@@ -151,7 +152,7 @@ def lib():
         for n in ("sf_sparse_gqa_workspace_bytes", "sf_pruned_ffn_workspace_bytes", "sf_encoder_workspace_bytes",
                   "sf_moe_ffn_workspace_bytes", "sf_pruned_ffn_fp8_workspace_bytes", "sf_encoder_fp8_workspace_bytes",
                   "sf_sparse_gqa_static_capacity", "sf_encoder_packed_workspace_bytes", "sf_linear_i8_workspace_bytes",
-                  "sf_pruned_ffn_i8_workspace_bytes"):
+                  "sf_pruned_ffn_i8_workspace_bytes", "sf_cross_gqa_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         for n in ("sf_num_active", "sf_ffn_padded", "sf_gate_scores_to_masks", "sf_compact_heads_channels",
                   "sf_sparse_gqa_forward", "sf_pruned_ffn_forward", "sf_encoder_forward", "sf_profile_begin",
@@ -162,7 +163,8 @@ def lib():
                   "sf_active_projection_rows", "sf_compact_proj_fp8", "sf_encoder_forward_fp8", "sf_proj_fp8_padded",
                   "sf_presence_to_key_valid", "sf_sparse_gqa_forward_static", "sf_token_pack_rows_max",
                   "sf_token_pack", "sf_token_unpack", "sf_encoder_forward_packed", "sf_sparse_gqa_plan",
-                  "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_forward", "sf_compact_ffn_i8", "sf_pruned_ffn_i8_forward"):
+                  "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_forward", "sf_compact_ffn_i8", "sf_pruned_ffn_i8_forward",
+                  "sf_cross_gqa_forward"):
             getattr(L, n).restype = C.c_int32
         L.sf_gemm_kernel.argtypes = [C.POINTER(SfDesc)] + [C.c_int32] * 4
         L.sf_sparse_gqa_plan.argtypes = [C.POINTER(SfDesc), C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
@@ -244,6 +246,10 @@ def lib():
         L.sf_pruned_ffn_i8_workspace_bytes.argtypes = [C.POINTER(SfDesc), C.c_int32]
         L.sf_pruned_ffn_i8_forward.argtypes = [C.POINTER(SfDesc), C.POINTER(SfFfnI8), C.c_void_p, C.c_void_p, C.c_int32,
                                                C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sf_cross_gqa_workspace_bytes.argtypes = [C.POINTER(SfDesc), C.c_int32, C.c_int32, C.c_int32]
+        L.sf_cross_gqa_forward.argtypes = [C.POINTER(SfDesc), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, SfStrides, C.c_void_p,
+                                           SfStrides, C.c_void_p, SfStrides, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                           C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
         L.sf_profile_begin.argtypes = [C.c_int32, C.c_int32]
         L.sf_profile_end.argtypes = [C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_float)]
         L.sf_num_active.argtypes = [C.POINTER(SfDesc)]
@@ -568,6 +574,34 @@ def sparse_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.
     if sel is not None:
         sel = sel[:, :, :U]
     return O, sel, score
+
+
+def cross_gqa_workspace_bytes(desc: SfDesc, Lk: int, nH: int, nG: int) -> int:
+    return int(lib().sf_cross_gqa_workspace_bytes(C.byref(desc), int(Lk), int(nH), int(nG)))
+
+
+def cross_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, head_group: torch.Tensor,
+                      pattern_id: Optional[torch.Tensor] = None, key_valid: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Q [B,nH,Lq,dh] over K, V [B,nG,Lk,dh] (last dimension contiguous, any other strides), desc with L = Lq;
+    head_group [n_maps,nH] int32, key_valid [B,Lk] u8.  Returns O [B,Lq,nH*dh] (out: row stride any)."""
+    B, nH, Lq, dh = Q.shape
+    nG, Lk, dt = K.shape[1], K.shape[2], Q.dtype
+    assert (desc.B, desc.L, desc.dh) == (B, Lq, dh) and dt == torch_dtype(desc.dtype) == K.dtype == V.dtype
+    assert K.shape == V.shape and K.shape[0] == B and K.shape[3] == dh
+    assert head_group.dtype == torch.int32 and head_group.is_contiguous() and head_group.shape[-1] == nH
+    assert pattern_id is None or (pattern_id.dtype == torch.int32 and pattern_id.is_contiguous() and pattern_id.numel() == B)
+    assert key_valid is None or (key_valid.dtype == torch.uint8 and key_valid.is_contiguous() and tuple(key_valid.shape) == (B, Lk))
+    if out is None:
+        out = torch.empty((B, Lq, nH * dh), dtype=dt, device=Q.device)
+    assert out.dtype == dt and tuple(out.shape) == (B, Lq, nH * dh) and out.stride(2) == 1 and (B == 1 or out.stride(0) == Lq * out.stride(1))
+    if ws is None:
+        ws = workspace(cross_gqa_workspace_bytes(desc, Lk, nH, nG), Q.device)
+    _check(lib().sf_cross_gqa_forward(C.byref(desc), nH, nG, Lk, Q.data_ptr(), _strides4(Q), K.data_ptr(), _strides4(K), V.data_ptr(),
+                                      _strides4(V), head_group.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
+                                      None if key_valid is None else key_valid.data_ptr(), out.data_ptr(), out.stride(1), ws.data_ptr(),
+                                      ws.numel(), _stream_of(Q)), "sf_cross_gqa_forward")
+    return out
 
 
 def sparse_gqa_static_capacity() -> int:
