@@ -763,6 +763,23 @@ int32_t sf_moe_ffn_forward(const sf_desc *desc, const sf_moe_compact *moe_host, 
                            float *weight_out, float *logit_out, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* The same block for a few tokens (at most SF_MOE_FEW_TOKENS in all, B*L: the
+ * read-out tokens of a batch, a single one) in two launches that read the chosen
+ * experts' weights once.  Arguments, routing rules and outputs as above (Y may not
+ * alias X), with these differences: nothing is rounded between X and Y - the
+ * LayerNorm output and the hidden activations stay in fp32 -, so logits, and with
+ * them a choice between two almost equal experts, may differ from
+ * sf_moe_ffn_forward's in the places that a 16-bit xn moves; d_model a
+ * multiple of 8, at most 1024; X, Y, Wr, W1 and W2T on 16 bytes.  binary16: hidden
+ * activations must fit the type, as above. */
+#define SF_MOE_FEW_TOKENS 64
+size_t sf_moe_ffn_few_workspace_bytes(const sf_desc *desc, const sf_moe_compact *moe_host);
+int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_compact *moe_host, const void *X,
+                               const int32_t *pattern_id, int32_t pre_ln, int32_t add_residual,
+                               const int32_t *forced_route, void *Y, int32_t *route_out,
+                               float *weight_out, float *logit_out, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
 /* ------------------------------------------------------------------------
  * SentryGate on the device (plan construction; fp32 whatever the model dtype).
  *

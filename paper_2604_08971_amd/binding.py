@@ -40,7 +40,8 @@ EXPORTS = ["sf_last_error", "sf_num_active", "sf_ffn_padded", "sf_gate_scores_to
            "sf_encoder_packed_workspace_bytes", "sf_encoder_forward_packed", "sf_sparse_gqa_plan",
            "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_workspace_bytes", "sf_linear_i8_forward",
            "sf_compact_ffn_i8", "sf_pruned_ffn_i8_workspace_bytes", "sf_pruned_ffn_i8_forward",
-           "sf_cross_gqa_workspace_bytes", "sf_cross_gqa_forward"]
+           "sf_cross_gqa_workspace_bytes", "sf_cross_gqa_forward", "sf_moe_ffn_few_workspace_bytes",
+           "sf_moe_ffn_few_forward"]
 SF_GATE_RELU, SF_GATE_TANH = 0, 1
 SF_KERNEL_GEMM, SF_KERNEL_SCORE, SF_KERNEL_ATTEND, SF_KERNEL_ATTENTION, SF_KERNEL_LAYERNORM = 0, 1, 2, 3, 4
 
@@ -152,7 +153,8 @@ def lib():
         for n in ("sf_sparse_gqa_workspace_bytes", "sf_pruned_ffn_workspace_bytes", "sf_encoder_workspace_bytes",
                   "sf_moe_ffn_workspace_bytes", "sf_pruned_ffn_fp8_workspace_bytes", "sf_encoder_fp8_workspace_bytes",
                   "sf_sparse_gqa_static_capacity", "sf_encoder_packed_workspace_bytes", "sf_linear_i8_workspace_bytes",
-                  "sf_pruned_ffn_i8_workspace_bytes", "sf_cross_gqa_workspace_bytes"):
+                  "sf_pruned_ffn_i8_workspace_bytes", "sf_cross_gqa_workspace_bytes",
+                  "sf_moe_ffn_few_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         for n in ("sf_num_active", "sf_ffn_padded", "sf_gate_scores_to_masks", "sf_compact_heads_channels",
                   "sf_sparse_gqa_forward", "sf_pruned_ffn_forward", "sf_encoder_forward", "sf_profile_begin",
@@ -164,7 +166,7 @@ def lib():
                   "sf_presence_to_key_valid", "sf_sparse_gqa_forward_static", "sf_token_pack_rows_max",
                   "sf_token_pack", "sf_token_unpack", "sf_encoder_forward_packed", "sf_sparse_gqa_plan",
                   "sf_gemm_kernel", "sf_quantize_i8_rows", "sf_linear_i8_forward", "sf_compact_ffn_i8", "sf_pruned_ffn_i8_forward",
-                  "sf_cross_gqa_forward"):
+                  "sf_cross_gqa_forward", "sf_moe_ffn_few_forward"):
             getattr(L, n).restype = C.c_int32
         L.sf_gemm_kernel.argtypes = [C.POINTER(SfDesc)] + [C.c_int32] * 4
         L.sf_sparse_gqa_plan.argtypes = [C.POINTER(SfDesc), C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
@@ -231,6 +233,8 @@ def lib():
         L.sf_moe_ffn_forward.argtypes = [C.POINTER(SfDesc), C.POINTER(SfMoeCompact), C.c_void_p, C.c_void_p, C.c_int32,
                                          C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sf_moe_ffn_few_workspace_bytes.argtypes = L.sf_moe_ffn_workspace_bytes.argtypes
+        L.sf_moe_ffn_few_forward.argtypes = L.sf_moe_ffn_forward.argtypes
         L.sf_gate_eval.argtypes = [C.POINTER(SfDesc), C.POINTER(SfGateParams), C.c_void_p, C.c_void_p, C.c_void_p,
                                    C.c_void_p]
         L.sf_budget_search.argtypes = [C.POINTER(SfDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
@@ -928,6 +932,39 @@ def moe_ffn_forward(desc: SfDesc, moe: CompactMoe, X: torch.Tensor, pattern_id: 
                                   int(add_residual), _ptr(forced_route), _ptr(Y), _ptr(route), _ptr(weight),
                                   _ptr(logit), _ptr(ws), ws.numel(), _stream())
     _check(rc, "sf_moe_ffn_forward")
+    return (Y, route, weight, logit) if want_route else Y
+
+
+MOE_FEW_TOKENS = 64
+
+
+def moe_ffn_few_workspace_bytes(desc: SfDesc, moe: CompactMoe) -> int:
+    return int(lib().sf_moe_ffn_few_workspace_bytes(C.byref(desc), C.byref(moe.struct)))
+
+
+def moe_ffn_few_forward(desc: SfDesc, moe: CompactMoe, X: torch.Tensor, pattern_id: Optional[torch.Tensor] = None,
+                        pre_ln: bool = True, add_residual: bool = True, forced_route: Optional[torch.Tensor] = None,
+                        want_route: bool = False, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """moe_ffn_forward for at most MOE_FEW_TOKENS rows of X [B*L, d], in two launches.  Returns what it returns."""
+    rows = desc.B * desc.L
+    assert X.is_contiguous() and X.dtype == moe.W1.dtype == torch_dtype(desc.dtype) and X.numel() == rows * desc.d_model
+    assert pattern_id is None or (pattern_id.dtype == torch.int32 and pattern_id.is_contiguous() and pattern_id.numel() == desc.B)
+    Y = torch.empty_like(X) if out is None else out
+    assert Y.is_contiguous() and Y.dtype == X.dtype and Y.numel() == X.numel()
+    dev, route, weight, logit, fr = X.device, None, None, None, None
+    if want_route:
+        route = torch.empty((rows, moe.top_k), dtype=torch.int32, device=dev)
+        weight = torch.empty((rows, moe.top_k), dtype=torch.float32, device=dev)
+        logit = torch.empty((rows, moe.E), dtype=torch.float32, device=dev)
+    if forced_route is not None:
+        assert forced_route.dtype == torch.int32 and forced_route.is_contiguous()
+        assert tuple(forced_route.shape) == (rows, moe.top_k)
+        fr = forced_route.data_ptr()
+    if ws is None:
+        ws = workspace(moe_ffn_few_workspace_bytes(desc, moe), dev)
+    _check(lib().sf_moe_ffn_few_forward(C.byref(desc), C.byref(moe.struct), X.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
+                                        pre_ln, add_residual, fr, Y.data_ptr(), *[None if t is None else t.data_ptr() for t in (route, weight, logit)],
+                                        ws.data_ptr(), ws.numel(), _stream_of(X)), "sf_moe_ffn_few_forward")
     return (Y, route, weight, logit) if want_route else Y
 
 

@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libsentryfuse.so")
 LIB_F16 = os.path.join(HERE, "libsentryfuse_f16.so")
 
 SOURCES = ["api.hip", "masks.hip", "compact.hip", "gemm_bf16.hip", "gemm_bf16_tile.hip", "gemm_bf16_rows.hip", "gemm_bf16_ws.hip", "gemm_f32.hip", "moe.hip", "gate.hip", "fp8_ffn.hip", "tokens.hip", "lazy_proj.hip", "fp8_proj.hip",
-           "i8_rows.hip", "i8_gemm.hip", "i8_linear.hip", "cross.hip",
+           "i8_rows.hip", "i8_gemm.hip", "i8_linear.hip", "cross.hip", "moe_few.hip",
            "attention_common.hip", "attention_bf16.hip", "attention_short.hip", "ceilings.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
