@@ -2,14 +2,14 @@
 //
 //   up:    every workgroup normalises the tokens and routes them for itself (LayerNorm, logits, Top-k), then takes channels of one of the
 //          chosen (pattern, expert) pairs: hidden rows in fp32, one per (token, slot)
-//   down:  features of one pair over a range of its channels; the workgroup that finishes a run of features last adds up the slots,
-//          in their order, with their weights, and the residual
+//   down:  four features of every token: the pairs' products, the slots' sum with their weights in the order of the slots, the residual
 //
-// The products run on the matrix cores, weights as the first operand, sixteen tokens as the second.  An activation goes in as a sum of
+// The products run on the matrix cores, weights as the first operand, tokens as the second.  An activation goes in as a sum of
 // 16-bit terms, so that nothing is rounded on the way: two terms (16 bits in bfloat16, 22 in binary16) for the experts' products, three for
 // the logits, whose order decides.  fp32 models take the fp32 instruction.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "gemm.hpp"
 
@@ -17,20 +17,26 @@ namespace sf {
 
 namespace {
 
-constexpr int FEW = SF_MOE_FEW_TOKENS, TILE_T = 16, MAX_D = 1024, MAX_SEGS = 4096, STEPS = MAX_D / 32 / 4;      // K steps of 32 that a wave of four owns
+constexpr int FEW = SF_MOE_FEW_TOKENS, TILE_T = 16, MAX_D = 1024, WAVES = 8, NT = WAVES * 64, STEPS = MAX_D / 32 / WAVES;      // K steps of 32 of a wave
+constexpr int XT_BYTES = 100 * 1024;                        // LDS that normalised tokens may take: all of them up to here, else sixteen at a time
 #ifdef SF_HALF_F16
 #define SF_MFMA_16X16 __builtin_amdgcn_mfma_f32_16x16x32_f16
+#define SF_MFMA_4X4(w, x, acc) __builtin_amdgcn_mfma_f32_4x4x4f16(w, x, acc, 0, 0, 0)
 #else
 #define SF_MFMA_16X16 __builtin_amdgcn_mfma_f32_16x16x32_bf16
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+#define SF_MFMA_4X4(w, x, acc) __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, w), __builtin_bit_cast(s16x4, x), acc, 0, 0, 0)
 #endif
 
 struct FewMoe {
     const void *X, *Wr, *br, *ln_g, *ln_b, *W1, *b1, *W2T, *b2x;
     const int32_t *pattern_id, *forced, *k_ffn;
     int T, L, d, E, P, top_k, ffn_pad, Fp, act; float eps; int add_residual;
-    int segs, slices, parts;                                 // most pairs in use; workgroups of a pair (up), ranges of its channels (down)
-    int32_t *route; float *weight; int32_t *done; float *hid, *z;      // workspace: [T k] (-1: listed again in a later slot), [T k],
-                                                             // [features / 16], [T k, Fp], [parts, T k, d]
+    int segs, by_slot, slices, parts;                        // pairs looked at (by_slot: those of each (token, slot), else all there are);
+                                                             // workgroups of a pair (up), ranges of its channels (down)
+    int tile_rows;                                           // normalised tokens in LDS at a time
+    int32_t *route; float *weight;                           // workspace: [T k] (-1: listed again in a later slot), [T k]
+    void *hid;                                               // [T k, Fp] fp32, or the two terms [2, T k, Fp] in 16 bits
     void *Y; int32_t *route_out; float *weight_out, *logit_out;
 };
 
@@ -87,52 +93,31 @@ __device__ __forceinline__ float activated(int act, float z)
     return sizeof(T) == 4 ? 0.5f * z * (1.0f + erff(z * 0.70710678f)) : gelu_erf(z);
 }
 
-// The pairs in use: seg of every (token, slot), whether it is the first of its seg, and the tokens of the n-th seg in use
-struct Pairs {
-    short slot[FEW];                                         // of the seg looked for: its (token, slot) numbers
-    int n, seg;
-};
 __device__ __forceinline__ int pattern_of(const FewMoe &a, int t)
 {
     return a.pattern_id ? min(max(a.pattern_id[t / a.L], 0), a.P - 1) : 0;
 }
-// route(i): the expert of (token, slot) i, negative where it does not count; first: LDS for P E numbers, the lowest (token, slot) of a pair.
-// All 256 threads.  false: fewer than `nth` + 1 pairs are in use
-template <class Route>
-__device__ bool find_pairs(const FewMoe &a, Pairs &p, int *first, int nth, Route route)
+
+// The `nth` pair looked at: its number (pattern E + expert), and the (token, slot) in which the lane's token chose it or -1.  by_slot: the pair of
+// (token, slot) nth, unless an earlier one is the same.  pick: the experts of the lane's token, negative where they do not count.  Registers of
+// one wave only.
+struct Pair { int seg, at; };
+__device__ __forceinline__ Pair find_pair(const FewMoe &a, const int (&pick)[8], int pattern, int nth)
 {
-    const int n = a.T * a.top_k, lane = threadIdx.x & 63;
-    for (int i = threadIdx.x; i < a.P * a.E; i += 256) first[i] = 0x7fffffff;
-    if (threadIdx.x == 0) p.seg = -1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const int e = route(i);
-        if (e >= 0) atomicMin(&first[pattern_of(a, i / a.top_k) * a.E + e], i);
+    const int lane = threadIdx.x & 63;
+    Pair p{nth, -1};
+    if (a.by_slot) {
+        const int t = nth / a.top_k, s = nth - t * a.top_k;
+        int e = -1;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) e = q == s ? pick[q] : e;
+        e = __builtin_amdgcn_readlane(e, t);
+        p.seg = e < 0 ? -1 : __builtin_amdgcn_readlane(pattern, t) * a.E + e;
     }
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        int before = 0;
-        for (int i0 = 0; i0 < n && before <= nth; i0 += 64) {
-            const int i = i0 + lane, e = i < n ? route(i) : -1;
-            const int s = e >= 0 ? pattern_of(a, i / a.top_k) * a.E + e : -1;
-            const uint64_t is_first = __ballot(s >= 0 && first[s < 0 ? 0 : s] == i);
-            const int rank = before + __popcll(is_first & ((1ull << lane) - 1));
-            if ((is_first >> lane & 1) && rank == nth) p.seg = s;
-            before += __popcll(is_first);
-        }
-    }
-    __syncthreads();
-    if (p.seg < 0) return false;
-    if (threadIdx.x < 64) {
-        int at = -1;
-        if (lane < a.T && pattern_of(a, lane) == p.seg / a.E)
-            for (int s = 0; s < a.top_k; ++s) if (route(lane * a.top_k + s) == p.seg % a.E) at = lane * a.top_k + s;
-        const uint64_t m = __ballot(at >= 0);
-        if (at >= 0) p.slot[__popcll(m & ((1ull << lane) - 1))] = (short)at;
-        if (lane == 0) p.n = __popcll(m);
-    }
-    __syncthreads();
-    return true;
+    if (p.seg < 0 || pattern != p.seg / a.E) return p;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) if (s < a.top_k && pick[s] == p.seg % a.E) p.at = lane * a.top_k + s;
+    return p;
 }
 
 // Channels of seg's expert, padded as its weights are
@@ -143,85 +128,149 @@ __device__ __forceinline__ int width_of(const FewMoe &a, int seg)
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void moe_few_up_kernel(FewMoe a)
+__global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 {
-    extern __shared__ __attribute__((aligned(16))) float xt[];         // [16][dp + 4] normalised tokens: rows 16 bytes apart over the banks
-    __shared__ Pairs pairs;
-    __shared__ float mean[FEW], rstd[FEW], red[4][64][TILE_T + 1];
-    static_assert(sizeof(red) >= MAX_SEGS * sizeof(int), "find_pairs");
-    __shared__ signed char pick[FEW * 8];
+    // [tile_rows][dp + 4] normalised tokens (rows 16 bytes apart over the banks), then partial sums [8][E or 32][17], then logits [T][E + 1]
+    extern __shared__ __attribute__((aligned(16))) float xt[];
+    __shared__ float mean[FEW], rstd[FEW];
+    __shared__ short slots[WAVES][FEW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kq = (lane >> 4) * 8;
-    const int d = a.d, dp = (d + 31) / 32 * 32, ld = dp + 4, steps = dp / 32, lgs = a.E + 1;
-    float *lg = xt + TILE_T * ld;                            // [T][E + 1]
+    const int d = a.d, dp = (d + 31) / 32 * 32, ld = dp + 4, steps = dp / 32, lgs = a.E + 1, tiles_e = (a.E + 15) / 16;
+    const int red_e = tiles_e < 2 ? 32 : tiles_e * 16;
+    float *red = xt + a.tile_rows * ld, *lg = red + WAVES * red_e * (TILE_T + 1);
+    auto part = [&](int w, int e, int r) -> float & { return red[(w * red_e + e) * (TILE_T + 1) + r]; };
     const T *X = (const T *)a.X;
-    // token t normalised into row r of xt; statistics the first time
-    auto normalise = [&](int t, int r, bool first) {
-        const T *x = X + (int64_t)t * d;
-        float v[MAX_D / 64], sum = 0.f;
+    constexpr int NCH = MAX_D / 512;
+    float gm[NCH][8], bt[NCH][8];
+    auto eight = [&](const T *p, int j, float *v) {
+        const int at = (lane + j * 64) * 8;
+        const auto q = load8(p + at, at < d);
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int j = 0; j < MAX_D / 64; ++j) {
-            const int at = lane + j * 64;
-            v[j] = at < d ? to_f32(x[at]) : 0.f;
-            sum += v[j];
+            for (int e = 0; e < 8; ++e) v[e] = (float)q[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = q.a[e]; v[4 + e] = q.b[e]; }
         }
-        if (a.ln_g) {
-            float m, inv;
-            if (first) {
-                m = wave_sum(sum) / d;
-                float q = 0.f;
-#pragma unroll
-                for (int j = 0; j < MAX_D / 64; ++j) if (lane + j * 64 < d) q = fmaf(v[j] - m, v[j] - m, q);
-                inv = 1.0f / sqrtf(wave_sum(q) / d + a.eps);
-                if (lane == 0) { mean[t] = m; rstd[t] = inv; }
-            } else { m = mean[t]; inv = rstd[t]; }
-#pragma unroll
-            for (int j = 0; j < MAX_D / 64; ++j) {
-                const int at = lane + j * 64;
-                if (at < d) v[j] = fmaf((v[j] - m) * inv, to_f32(((const T *)a.ln_g)[at]), to_f32(((const T *)a.ln_b)[at]));
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < MAX_D / 64; ++j) if (lane + j * 64 < dp) xt[r * ld + lane + j * 64] = v[j];
     };
-    auto clear = [&](int r) { for (int at = lane; at < dp; at += 64) xt[r * ld + at] = 0.f; };
+    if (a.ln_g) {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) { eight((const T *)a.ln_g, j, gm[j]); eight((const T *)a.ln_b, j, bt[j]); }
+    }
+    // tokens of(0) .. of(n - 1) normalised into rows r0 .. of xt; statistics the first time.  A wave takes two of them at once.
+    auto normalise = [&](int n, int r0, bool first, auto of) {
+        for (int i = wave; i < n; i += 2 * WAVES) {
+            float v[2][NCH][8];
+            int t[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int k = i + u * WAVES;
+                t[u] = of(k < n ? k : i);
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) eight(X + (int64_t)t[u] * d, j, v[u][j]);
+            }
+            if (a.ln_g) {
+                float m[2], inv[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (first) {
+                        float sum = 0.f, q = 0.f;
+#pragma unroll
+                        for (int j = 0; j < NCH; ++j)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) sum += v[u][j][e];
+                        m[u] = wave_sum(sum) / d;
+#pragma unroll
+                        for (int j = 0; j < NCH; ++j)
+                            if ((lane + j * 64) * 8 < d) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) q = fmaf(v[u][j][e] - m[u], v[u][j][e] - m[u], q);
+                            }
+                        inv[u] = 1.0f / sqrtf(wave_sum(q) / d + a.eps);
+                        if (lane == 0) { mean[t[u]] = m[u]; rstd[t[u]] = inv[u]; }
+                    } else { m[u] = mean[t[u]]; inv[u] = rstd[t[u]]; }
+#pragma unroll
+                    for (int j = 0; j < NCH; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][j][e] = fmaf((v[u][j][e] - m[u]) * inv[u], gm[j][e], bt[j][e]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) {
+                    const int at = (lane + j * 64) * 8;
+                    if (i + u * WAVES >= n || at >= dp) continue;
+                    float *o = xt + (r0 + i + u * WAVES) * ld + at;
+                    const bool in = at < d;                  // zeros from d to the next multiple of 32
+                    *reinterpret_cast<f32x4 *>(o) = in ? f32x4{v[u][j][0], v[u][j][1], v[u][j][2], v[u][j][3]} : f32x4{0.f, 0.f, 0.f, 0.f};
+                    *reinterpret_cast<f32x4 *>(o + 4) = in ? f32x4{v[u][j][4], v[u][j][5], v[u][j][6], v[u][j][7]} : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+        }
+    };
+    // K step s of row r of xt, as TERMS terms
+    auto operand = [&](int r, int s, auto terms) {
+        float v[8];
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        const float *p = xt + r * ld + s * 32 + kq;
+        const f32x4 lo = r >= 0 ? *reinterpret_cast<const f32x4 *>(p) : zero, hi = r >= 0 ? *reinterpret_cast<const f32x4 *>(p + 4) : zero;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+        return Operand<T>::template split<decltype(terms)::value>(v);
+    };
 
     // ---- route
+    const bool resident = a.T <= a.tile_rows;
+    if (resident) {
+        normalise(a.T, 0, true, [](int i) { return i; });
+        __syncthreads();
+    }
     for (int t0 = 0; t0 < a.T; t0 += TILE_T) {
-        __syncthreads();
-        for (int r = wave; r < TILE_T; r += 4) {
-            if (t0 + r < a.T) normalise(t0 + r, r, true);
-            else clear(r);
+        const int n = a.T - t0 < TILE_T ? a.T - t0 : TILE_T;
+        if (!resident) {
+            normalise(n, 0, true, [&](int i) { return t0 + i; });
+            __syncthreads();
         }
-        __syncthreads();
         f32x4 acc[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int s = wave; s < steps; s += 4) {
-            const auto x = Operand<T>::template split<3>(xt + c * ld + s * 32 + kq);
+        for (int s = wave; s < steps; s += WAVES) {
+            typename Weights<T>::type w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (i * 16 >= a.E) break;
                 const int e = i * 16 + c;
-                acc[i] = x.template times<3>(load8((const T *)a.Wr + (int64_t)e * d + s * 32 + kq, e < a.E && s * 32 + kq < d), acc[i]);
+                if (i < tiles_e) w[i] = load8((const T *)a.Wr + (int64_t)e * d + s * 32 + kq, e < a.E && s * 32 + kq < d);
             }
+            const auto x = operand(c < n ? (resident ? t0 + c : c) : -1, s, std::integral_constant<int, 3>());
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (i < tiles_e) acc[i] = x.template times<3>(w[i], acc[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            if (i >= tiles_e) break;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][i * 16 + (lane >> 4) * 4 + e][c] = acc[i][e];
+            for (int e = 0; e < 4; ++e) part(wave, i * 16 + (lane >> 4) * 4 + e, c) = acc[i][e];
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < a.E * TILE_T; i += 256) {
-            const int e = i / TILE_T, r = i % TILE_T;
-            const float *p = &red[0][e][r];
-            constexpr int W = 64 * (TILE_T + 1);
-            if (t0 + r < a.T) lg[(t0 + r) * lgs + e] = (p[0] + p[W]) + (p[2 * W] + p[3 * W]) + (a.br ? to_f32(((const T *)a.br)[e]) : 0.f);
+        for (int i = threadIdx.x; i < a.E * n; i += NT) {
+            const int e = i / n, r = i - e * n;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) sum += part(w, e, r);
+            lg[(t0 + r) * lgs + e] = sum + (a.br ? to_f32(((const T *)a.br)[e]) : 0.f);
         }
+        __syncthreads();
     }
-    __syncthreads();
+    // Every wave chooses for all tokens, a lane each.  Ties go to the lower expert, a NaN ranks below every number; an expert that the caller
+    // lists twice counts in its last slot.
     const bool one = blockIdx.x == 0;
-    if ((int)threadIdx.x < a.T) {
-        // ties go to the lower expert, a NaN ranks below every number; an expert that the caller lists twice counts in its last slot
-        const int t = threadIdx.x;
+    int pick[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) pick[s] = -1;
+    const int pattern = lane < a.T ? pattern_of(a, lane) : 0;
+    if (lane < a.T) {
+        const int t = lane;
+        const float *my = lg + t * lgs;
         unsigned long long taken = 0;
         float most = -INFINITY, den = 0.f, v[8];
         int who[8];
@@ -234,13 +283,18 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(FewMoe a)
             float bv = -INFINITY;
             if (a.forced) {
                 be = min(max(a.forced[t * a.top_k + s], 0), a.E - 1);
-                bv = lg[t * lgs + be];
+                bv = my[be];
                 bv = bv == bv ? bv : -INFINITY;
             } else {
-                for (int e = 0; e < a.E; ++e) {
-                    float u = lg[t * lgs + e];
-                    u = u == u ? u : -INFINITY;
-                    if (!(taken >> e & 1) && (be < 0 || u > bv)) { be = e; bv = u; }
+                for (int e0 = 0; e0 < a.E; e0 += 8) {
+                    float u[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e] = my[e0 + e < a.E ? e0 + e : 0];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = u[e] == u[e] ? u[e] : -INFINITY;
+                        if (e0 + e < a.E && !(taken >> (e0 + e) & 1) && (be < 0 || x > bv)) { be = e0 + e; bv = x; }
+                    }
                 }
                 taken |= 1ull << be;
             }
@@ -254,170 +308,195 @@ __global__ __launch_bounds__(256) void moe_few_up_kernel(FewMoe a)
 #pragma unroll
             for (int q = s + 1; q < 8; ++q) again[s] = again[s] || (q < a.top_k && who[q] == who[s]);
             if (!again[s]) most = fmaxf(most, v[s]);
+            pick[s] = again[s] ? -1 : who[s];
         }
+        if (one && wave == 0) {
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            v[s] = s < a.top_k && !again[s] ? expf(v[s] - most) : 0.f;
-            den += v[s];
-        }
+            for (int s = 0; s < 8; ++s) {
+                v[s] = s < a.top_k && !again[s] ? expf(v[s] - most) : 0.f;
+                den += v[s];
+            }
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            if (s >= a.top_k) continue;
-            const int i = t * a.top_k + s;
-            pick[i] = (signed char)(again[s] ? -1 : who[s]);
-            if (one) {
-                a.route[i] = pick[i];
+            for (int s = 0; s < 8; ++s) {
+                if (s >= a.top_k) continue;
+                const int i = t * a.top_k + s;
+                a.route[i] = pick[s];
                 a.weight[i] = v[s] / den;
                 if (a.route_out) a.route_out[i] = who[s];
                 if (a.weight_out) a.weight_out[i] = v[s] / den;
             }
         }
     }
-    if (one) {
-        if (a.logit_out) for (int i = threadIdx.x; i < a.T * a.E; i += 256) a.logit_out[i] = lg[i / a.E * lgs + i % a.E];
-        for (int i = threadIdx.x; i < (d + 15) / 16; i += 256) a.done[i] = 0;
-    }
-    __syncthreads();
-    if (!find_pairs(a, pairs, reinterpret_cast<int *>(red), blockIdx.x / a.slices, [&](int i) { return (int)pick[i]; })) return;
+    if (one && a.logit_out)
+        for (int i = threadIdx.x; i < a.T * a.E; i += NT) a.logit_out[i] = lg[i / a.E * lgs + i % a.E];
 
-    // ---- channels of the pair
-    const int seg = pairs.seg, groups = width_of(a, seg) / 16;
+    // ---- channels of a pair
+    const int nth = blockIdx.x / a.slices;
+    const Pair pair = find_pair(a, pick, pattern, nth);
+    const uint64_t chose = __ballot(pair.at >= 0);
+    if (!chose || (a.by_slot && __ballot(pair.at >= 0 && pair.at < nth))) return;
+    const int seg = pair.seg, n_all = __popcll(chose), groups = width_of(a, seg) / 16;
+    if (pair.at >= 0) slots[wave][__popcll(chose & ((1ull << lane) - 1))] = (short)pair.at;      // each wave for itself
     const T *W1 = (const T *)a.W1 + (int64_t)seg * a.Fp * d, *b1 = a.b1 ? (const T *)a.b1 + (int64_t)seg * a.Fp : nullptr;
-    const int g0 = blockIdx.x % a.slices;
-    for (int t0 = 0; t0 < (a.T <= TILE_T ? 1 : pairs.n); t0 += TILE_T) {
-        // up to sixteen tokens in all: they lie in xt already, and the columns of those that chose otherwise are not stored
-        const bool all = a.T <= TILE_T;
-        if (!all) {
-            __syncthreads();
-            for (int r = wave; r < TILE_T; r += 4) {
-                if (t0 + r < pairs.n) normalise(pairs.slot[t0 + r] / a.top_k, r, false);
-                else clear(r);
-            }
-            __syncthreads();
-        }
-        Operand<T> x[STEPS];
+    const int g0 = blockIdx.x % a.slices, r = (threadIdx.x >> 4) & 15, half = threadIdx.x >> 8, ch = threadIdx.x & 15;
+    typename Weights<T>::type w[STEPS];
+    auto fetch = [&](int g) {
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
-            const int s = wave + j * 4;
-            if (s < steps) x[j] = Operand<T>::template split<2>(xt + c * ld + s * 32 + kq);
+            const int k = (wave + j * WAVES) * 32 + kq;
+            w[j] = load8(W1 + (int64_t)(g * 16 + c) * d + k, g < groups && k < d);
         }
-        // (token, slot) that this thread stores, channel threadIdx.x % 16 of the group
-        const int r = threadIdx.x >> 4;
-        int mine = -1;
-        if (!all) { if (t0 + r < pairs.n) mine = pairs.slot[t0 + r]; }
-        else
-            for (int i = 0; i < pairs.n; ++i) if (pairs.slot[i] / a.top_k == r) mine = pairs.slot[i];
-        typename Weights<T>::type w[STEPS];
-        auto fetch = [&](int g) {
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                const int k = (wave + j * 4) * 32 + kq;
-                w[j] = load8(W1 + (int64_t)(g * 16 + c) * d + k, g < groups && k < d);
-            }
-        };
+    };
+    for (int t0 = 0; t0 < n_all; t0 += TILE_T) {
         fetch(g0);
+        const int n = n_all - t0 < TILE_T ? n_all - t0 : TILE_T;
+        if (!resident) {
+            __syncthreads();
+            normalise(n, 0, false, [&](int i) { return slots[wave][t0 + i] / a.top_k; });
+        }
+        __syncthreads();
+        const int row = c < n ? (resident ? slots[wave][t0 + c] / a.top_k : c) : -1;
+        Operand<T> x[STEPS];
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) if (wave + j * WAVES < steps) x[j] = operand(row, wave + j * WAVES, std::integral_constant<int, 2>());
+        const int mine = half == 0 && r < n ? slots[wave][t0 + r] : -1;      // (token, slot) whose channel ch this thread stores
         for (int g = g0, b = 0; g < groups; g += a.slices, b ^= 1) {
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < STEPS; ++j) if (wave + j * 4 < steps) acc = x[j].template times<2>(w[j], acc);
+            for (int j = 0; j < STEPS; ++j) if (wave + j * WAVES < steps) acc = x[j].template times<2>(w[j], acc);
             fetch(g + a.slices);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][b * 16 + (lane >> 4) * 4 + e][c] = acc[e];
+            for (int e = 0; e < 4; ++e) part(wave, b * 16 + (lane >> 4) * 4 + e, c) = acc[e];
             __syncthreads();                                 // two buffers: the next round's values go into the other one
             if (mine >= 0) {
-                const int ch = threadIdx.x & 15, at = b * 16 + ch;
-                const float z = (red[0][at][r] + red[1][at][r]) + (red[2][at][r] + red[3][at][r]);
-                a.hid[(int64_t)mine * a.Fp + g * 16 + ch] = activated<T>(a.act, z + (b1 ? to_f32(b1[g * 16 + ch]) : 0.f));
+                float z = 0.f;
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) z += part(v, b * 16 + ch, r);
+                z = activated<T>(a.act, z + (b1 ? to_f32(b1[g * 16 + ch]) : 0.f));
+                const int64_t at = (int64_t)mine * a.Fp + g * 16 + ch;
+                if constexpr (sizeof(T) == 2) {
+                    const h16 hi = (h16)z;
+                    ((h16 *)a.hid)[at] = hi;
+                    ((h16 *)a.hid)[(int64_t)a.T * a.top_k * a.Fp + at] = (h16)(z - (float)hi);
+                } else ((float *)a.hid)[at] = z;
             }
         }
         __syncthreads();
     }
 }
 
+// Four features of all tokens.  A wave takes pairs in turn (or a range of a pair's channels) and multiplies in sixteen 4 x 4 blocks at once, four
+// features by four tokens, each over channels of its own: 16 bytes of a lane are eight channels of one feature.  The sums of the slots meet in LDS.
 template <class T>
-__global__ __launch_bounds__(256) void moe_few_down_kernel(FewMoe a)
+__global__ __launch_bounds__(NT) void moe_few_down_kernel(FewMoe a)
 {
-    __shared__ Pairs pairs;
-    __shared__ int first[MAX_SEGS];
-    __shared__ float red[4][16][TILE_T + 1];
-    __shared__ int last;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kq = (lane >> 4) * 8;
-    const int n0 = blockIdx.x * 16, d = a.d, pair_no = blockIdx.y / a.parts, part = blockIdx.y % a.parts, all = a.T * a.top_k;
-    if (find_pairs(a, pairs, first, pair_no, [&](int i) { return a.route[i]; })) {
-        const int seg = pairs.seg, steps = width_of(a, seg) / 32, from = steps * part / a.parts, to = steps * (part + 1) / a.parts;
-        const int n = n0 + c < d ? n0 + c : d - 1;
-        const T *W = (const T *)a.W2T + ((int64_t)seg * d + n) * a.Fp + kq;
-        for (int t0 = 0; t0 < pairs.n; t0 += TILE_T) {
-            const float *h = a.hid + (int64_t)pairs.slot[t0 + c < pairs.n ? t0 + c : t0] * a.Fp + kq;
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    extern __shared__ __attribute__((aligned(16))) float zs[];         // [parts][T k][4]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q4 = lane & 3, k8 = (lane >> 2) * 8;
+    const int n0 = blockIdx.x * 4, d = a.d, all = a.T * a.top_k;
+    const int pattern = lane < a.T ? pattern_of(a, lane) : 0;
+    int pick[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) pick[s] = lane < a.T && s < a.top_k ? a.route[lane * a.top_k + s] : -1;
+    for (int item = wave; item < a.segs * a.parts; item += WAVES) {
+        const int nth = item / a.parts, prt = item - nth * a.parts;
+        const Pair pair = find_pair(a, pick, pattern, nth);
+        uint64_t chose = __ballot(pair.at >= 0);
+        if (!chose || (a.by_slot && __ballot(pair.at >= 0 && pair.at < nth))) continue;
+        const int seg = pair.seg, width = width_of(a, seg), per = (width / 64 + a.parts - 1) / a.parts * 64;
+        const int from = prt * per, to = from + per < width ? from + per : width;
+        const T *W = (const T *)a.W2T + ((int64_t)seg * d + (n0 + q4 < d ? n0 + q4 : d - 1)) * a.Fp + k8;
+        while (chose) {                                      // up to sixteen tokens at a time
+            constexpr int TT = 4;
+            int at[TT], n = 0;
+#pragma unroll
+            for (int u = 0; u < TT; ++u) {
+                // the lane's token of the next four
+                uint64_t four = chose;
+                at[u] = -1;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    if (!four) break;
+                    const int t = __ffsll((unsigned long long)four) - 1;
+                    four &= four - 1;
+                    const int s = __builtin_amdgcn_readlane(pair.at, t);
+                    if (q4 == v) at[u] = s;
+                    ++n;
+                }
+                chose = four;
+            }
+            f32x4 acc[TT];
+#pragma unroll
+            for (int u = 0; u < TT; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
             constexpr int AHEAD = 4;
-            for (int s = from + wave; s < to; s += 4 * AHEAD) {
+            for (int k = from; k < to; k += 128 * AHEAD) {
                 typename Weights<T>::type w[AHEAD];
-                float v[AHEAD][8];
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) {
-                    const bool in = s + j * 4 < to;
-                    w[j] = load8(W + (s + j * 4) * 32, in);
+                for (int j = 0; j < AHEAD; ++j) w[j] = load8(W + k + j * 128, k + j * 128 + k8 < to);
 #pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        f32x4 q = {0.f, 0.f, 0.f, 0.f};
-                        if (in) q = *reinterpret_cast<const f32x4 *>(h + (s + j * 4) * 32 + e);
+                for (int u = 0; u < TT; ++u) {
+                    if (u * 4 >= n) break;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) v[j][e + k] = q[k];
+                    for (int j = 0; j < AHEAD; ++j) {
+                        const bool in = at[u] >= 0 && k + j * 128 + k8 < to;
+                        const int64_t h = (int64_t)at[u] * a.Fp + k + j * 128 + k8;
+                        if constexpr (sizeof(T) == 2) {
+                            const h16x8 hi = load8((const h16 *)a.hid + h, in), lo = load8((const h16 *)a.hid + (int64_t)all * a.Fp + h, in);
+#define SF_QUARTER(x, i) __builtin_shufflevector(x, x, (i) * 4, (i) * 4 + 1, (i) * 4 + 2, (i) * 4 + 3)
+                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 0), SF_QUARTER(lo, 0), acc[u]);
+                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 1), SF_QUARTER(lo, 1), acc[u]);
+                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 0), SF_QUARTER(hi, 0), acc[u]);
+                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 1), SF_QUARTER(hi, 1), acc[u]);
+#undef SF_QUARTER
+                        } else {
+                            const f32x8 v = load8((const float *)a.hid + h, in);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[u] = __builtin_amdgcn_mfma_f32_4x4x1f32(w[j].a[e], v.a[e], acc[u], 0, 0, 0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[u] = __builtin_amdgcn_mfma_f32_4x4x1f32(w[j].b[e], v.b[e], acc[u], 0, 0, 0);
+                        }
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < AHEAD; ++j) acc = Operand<T>::template split<2>(v[j]).template times<2>(w[j], acc);
             }
-            __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[wave][(lane >> 4) * 4 + e][c] = acc[e];
-            __syncthreads();
-            const int r = threadIdx.x >> 4, f = threadIdx.x & 15;
-            if (t0 + r < pairs.n && n0 + f < d)
-                a.z[((int64_t)part * all + pairs.slot[t0 + r]) * d + n0 + f] = (red[0][f][r] + red[1][f][r]) + (red[2][f][r] + red[3][f][r]);
+            for (int u = 0; u < TT; ++u) {
+                if (u * 4 >= n) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[u][e] = pair_sum<4>(pair_sum<8>(pair_sum<16>(pair_sum<32>(acc[u][e]))));
+                if (lane < 4 && at[u] >= 0) *reinterpret_cast<f32x4 *>(zs + (prt * all + at[u]) * 4) = acc[u];
+            }
         }
     }
-    // the last workgroup of these features adds the slots up
-    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(&a.done[blockIdx.x], 1) == (int)gridDim.y - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    const int f = threadIdx.x & 15;
-    if (n0 + f >= d) return;
-    for (int t = threadIdx.x >> 4; t < a.T; t += 16) {
-        float y = a.add_residual ? to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]) : 0.f;
-        const int p = pattern_of(a, t);
-        float sum = 0.f;
-        for (int s = 0; s < a.top_k; ++s) {
-            const int i = t * a.top_k + s, e = a.route[i];
-            if (e < 0) continue;
-            float z = a.b2x ? to_f32(((const T *)a.b2x)[((int64_t)p * a.E + e) * d + n0 + f]) : 0.f;
-            for (int q = 0; q < a.parts; ++q) z += a.z[((int64_t)q * all + i) * d + n0 + f];
-            sum = fmaf(a.weight[i], z, sum);
-        }
-        ((T *)a.Y)[(int64_t)t * d + n0 + f] = from_f32<T>(y + sum);
+    const int f = threadIdx.x & 3, t = threadIdx.x >> 2;
+    if (t >= a.T || n0 + f >= d) return;
+    const float x = a.add_residual ? to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]) : 0.f;
+    const int p = pattern_of(a, t);
+    float sum = 0.f;
+    for (int s = 0; s < a.top_k; ++s) {
+        const int i = t * a.top_k + s, e = a.route[i];
+        if (e < 0) continue;
+        float z = a.b2x ? to_f32(((const T *)a.b2x)[((int64_t)p * a.E + e) * d + n0 + f]) : 0.f;
+        for (int q = 0; q < a.parts; ++q) z += zs[(q * all + i) * 4 + f];
+        sum = fmaf(a.weight[i], z, sum);
     }
+    ((T *)a.Y)[(int64_t)t * d + n0 + f] = from_f32<T>(x + sum);
 }
 
-struct FewWs { int32_t *route; float *weight; int32_t *done; float *hid, *z; int Fp, segs, slices, parts; size_t bytes; };
+struct FewWs { int32_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, parts; size_t bytes; };
 FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
 {
     Carver c(ws);
     FewWs w{};
-    const int T = D.B * D.L, pairs = T * m.top_k, tiles = ceil_div(D.d, 16);
+    const int T = D.B * D.L, pairs = T * m.top_k;
     w.Fp = (int)align_up((size_t)m.k_ffn_max, (size_t)D.ffn_pad);
-    w.segs = pairs < D.P * m.n_experts ? pairs : D.P * m.n_experts;
-    // two workgroups per compute unit: each routes for itself, so more of them would do that more often
-    w.slices = std::min(w.Fp / 16, std::max(1, 512 / w.segs));
-    w.parts = std::min(8, std::max(1, 512 / (w.segs * tiles)));
+    w.by_slot = pairs < D.P * m.n_experts;
+    w.segs = w.by_slot ? pairs : D.P * m.n_experts;
+    // a workgroup per compute unit: each routes for itself, so more of them would do that more often
+    w.slices = std::min(w.Fp / 16, std::max(1, 256 / w.segs));
+    w.parts = std::max(1, WAVES / w.segs);
     w.route = c.take<int32_t>((size_t)pairs);
     w.weight = c.take<float>((size_t)pairs);
-    w.done = c.take<int32_t>((size_t)tiles);
     w.hid = c.take<float>((size_t)pairs * w.Fp);
-    w.z = c.take<float>((size_t)w.parts * pairs * D.d);
     w.bytes = c.off;
     return w;
 }
@@ -430,7 +509,7 @@ int32_t check_few(const Dims &D, const sf_moe_compact *m)
     if (m->k_ffn_max < 1 || m->k_ffn_max > D.F) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: k_ffn_max out of range");
     if (!m->k_ffn) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: k_ffn (device keep counts) missing");
     if ((int64_t)D.B * D.L > FEW) return fail(SF_ERR_SHAPE, "moe_ffn_few: at most %d tokens (sf_moe_ffn_forward takes any number)", FEW);
-    if ((int64_t)D.P * m->n_experts > MAX_SEGS) return fail(SF_ERR_SHAPE, "moe_ffn_few: more than %d (pattern, expert) pairs", MAX_SEGS);
+    if ((int64_t)D.P * m->n_experts > 4096) return fail(SF_ERR_SHAPE, "moe_ffn_few: more than 4096 (pattern, expert) pairs");
     if (D.d % 8 || D.d > MAX_D) return fail(SF_ERR_SHAPE, "moe_ffn_few: d_model must be a multiple of 8, at most %d", MAX_D);
     return SF_OK;
 }
@@ -469,22 +548,26 @@ extern "C" int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_comp
     a.pattern_id = D.P > 1 ? pattern_id : nullptr; a.forced = forced_route; a.k_ffn = m->k_ffn;
     a.T = D.B * D.L; a.L = D.L; a.d = D.d; a.E = m->n_experts; a.P = D.P; a.top_k = m->top_k; a.ffn_pad = D.ffn_pad; a.Fp = w.Fp;
     a.act = D.act == SF_GELU_ERF ? ACT_GELU : ACT_RELU; a.eps = D.eps; a.add_residual = add_residual;
-    a.segs = w.segs; a.slices = w.slices; a.parts = w.parts;
-    a.route = w.route; a.weight = w.weight; a.done = w.done; a.hid = w.hid; a.z = w.z;
+    a.segs = w.segs; a.by_slot = w.by_slot; a.slices = w.slices; a.parts = w.parts;
+    a.route = w.route; a.weight = w.weight; a.hid = w.hid;
     a.Y = Y; a.route_out = route_out; a.weight_out = weight_out; a.logit_out = logit_out;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const dim3 up((unsigned)(w.segs * w.slices)), down((unsigned)ceil_div(D.d, 16), (unsigned)(w.segs * w.parts));
-    const size_t lds = ((size_t)TILE_T * (align_up((size_t)D.d, 32) + 4) + (size_t)a.T * (a.E + 1)) * sizeof(float);
+    const size_t row = (align_up((size_t)D.d, 32) + 4) * sizeof(float);
+    a.tile_rows = a.T * row <= XT_BYTES ? a.T : std::min(a.T, TILE_T);
+    const int red_e = std::max(32, (int)align_up((size_t)a.E, 16));
+    const size_t lds = a.tile_rows * row + ((size_t)WAVES * red_e * (TILE_T + 1) + (size_t)a.T * (a.E + 1)) * sizeof(float);
     const bool bf = D.dtype == SF_BF16;
     auto kern = bf ? moe_few_up_kernel<h16> : moe_few_up_kernel<float>;
     static std::atomic<bool> attr_set[2] = {{false}, {false}};      // setting the attribute twice is harmless
     if (!attr_set[bf]) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (TILE_T * (MAX_D + 4) + FEW * 65) * 4) != hipSuccess)
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024) != hipSuccess)
             return fail(SF_ERR_HIP, "moe_ffn_few: cannot reserve LDS");
         attr_set[bf] = true;
     }
-    hipLaunchKernelGGL(kern, up, dim3(256), lds, st, a);
-    if (bf) hipLaunchKernelGGL(moe_few_down_kernel<h16>, down, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(moe_few_down_kernel<float>, down, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(w.segs * w.slices)), dim3(NT), lds, st, a);
+    const dim3 down((unsigned)ceil_div(D.d, 4));
+    const size_t zs = (size_t)w.parts * a.T * a.top_k * 4 * sizeof(float);
+    if (bf) hipLaunchKernelGGL(moe_few_down_kernel<h16>, down, dim3(NT), zs, st, a);
+    else hipLaunchKernelGGL(moe_few_down_kernel<float>, down, dim3(NT), zs, st, a);
     return check_launch("moe_ffn_few_forward");
 }
