@@ -18,6 +18,7 @@ namespace sf {
 namespace {
 
 constexpr int FEW = SF_MOE_FEW_TOKENS, TILE_T = 16, MAX_D = 1024, WAVES = 8, NT = WAVES * 64, STEPS = MAX_D / 32 / WAVES;      // K steps of 32 of a wave
+constexpr int DOWN_WAVES = 16;
 constexpr int XT_BYTES = 100 * 1024;                        // LDS that normalised tokens may take: all of them up to here, else sixteen at a time
 #ifdef SF_HALF_F16
 #define SF_MFMA_16X16 __builtin_amdgcn_mfma_f32_16x16x32_f16
@@ -120,25 +121,31 @@ __device__ __forceinline__ Pair find_pair(const FewMoe &a, const int (&pick)[8],
     return p;
 }
 
-// Channels of seg's expert, padded as its weights are
-__device__ __forceinline__ int width_of(const FewMoe &a, int seg)
+// Channels of an expert, padded as its weights are
+__device__ __forceinline__ int width_of(const FewMoe &a, int kept)
 {
-    const int w = (a.k_ffn[seg % a.E] + a.ffn_pad - 1) / a.ffn_pad * a.ffn_pad;
+    const int w = (kept + a.ffn_pad - 1) / a.ffn_pad * a.ffn_pad;
     return w < a.Fp ? w : a.Fp;
 }
 
-template <class T>
+// G: runs of sixteen channels per round of a workgroup, so that its weights are on their way together
+template <class T, int G>
 __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 {
-    // [tile_rows][dp + 4] normalised tokens (rows 16 bytes apart over the banks), then partial sums [8][E or 32][17], then logits [T][E + 1]
+    // [tile_rows][dp + 4] normalised tokens (rows 16 bytes apart over the banks), then partial sums [8][64][17], then logits [T][E + 1]
     extern __shared__ __attribute__((aligned(16))) float xt[];
     __shared__ float mean[FEW], rstd[FEW];
     __shared__ short slots[WAVES][FEW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kq = (lane >> 4) * 8;
     const int d = a.d, dp = (d + 31) / 32 * 32, ld = dp + 4, steps = dp / 32, lgs = a.E + 1, tiles_e = (a.E + 15) / 16;
-    const int red_e = tiles_e < 2 ? 32 : tiles_e * 16;
-    float *red = xt + a.tile_rows * ld, *lg = red + WAVES * red_e * (TILE_T + 1);
-    auto part = [&](int w, int e, int r) -> float & { return red[(w * red_e + e) * (TILE_T + 1) + r]; };
+    float *red = xt + a.tile_rows * ld, *lg = red + WAVES * 64 * (TILE_T + 1);
+    auto part = [&](int w, int e, int r) -> float & { return red[(w * 64 + e) * (TILE_T + 1) + r]; };
+    // what does not depend on the tokens is on its way first
+    const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
+    const float bias_r = a.br && lane < a.E ? to_f32(((const T *)a.br)[lane]) : 0.f;
+    typename Weights<T>::type wr[STEPS];
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) wr[j] = load8((const T *)a.Wr + (int64_t)c * d + (wave + j * WAVES) * 32 + kq, c < a.E && (wave + j * WAVES) * 32 + kq < d);
     const T *X = (const T *)a.X;
     constexpr int NCH = MAX_D / 512;
     float gm[NCH][8], bt[NCH][8];
@@ -234,10 +241,14 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
         f32x4 acc[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int s = wave; s < steps; s += WAVES) {
-            typename Weights<T>::type w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < STEPS; ++j) {
+            const int s = wave + j * WAVES;
+            if (s >= steps) break;
+            typename Weights<T>::type w[4];
+            w[0] = wr[j];
+#pragma unroll
+            for (int i = 1; i < 4; ++i) {
                 const int e = i * 16 + c;
                 if (i < tiles_e) w[i] = load8((const T *)a.Wr + (int64_t)e * d + s * 32 + kq, e < a.E && s * 32 + kq < d);
             }
@@ -252,13 +263,13 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
             for (int e = 0; e < 4; ++e) part(wave, i * 16 + (lane >> 4) * 4 + e, c) = acc[i][e];
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < a.E * n; i += NT) {
-            const int e = i / n, r = i - e * n;
-            float sum = 0.f;
+        for (int r = wave; r < n; r += WAVES)                // a lane per expert
+            if (lane < a.E) {
+                float sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += part(w, e, r);
-            lg[(t0 + r) * lgs + e] = sum + (a.br ? to_f32(((const T *)a.br)[e]) : 0.f);
-        }
+                for (int w = 0; w < WAVES; ++w) sum += part(w, lane, r);
+                lg[(t0 + r) * lgs + lane] = sum + bias_r;
+            }
         __syncthreads();
     }
     // Every wave chooses for all tokens, a lane each.  Ties go to the lower expert, a NaN ranks below every number; an expert that the caller
@@ -267,7 +278,6 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     int pick[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) pick[s] = -1;
-    const int pattern = lane < a.T ? pattern_of(a, lane) : 0;
     if (lane < a.T) {
         const int t = lane;
         const float *my = lg + t * lgs;
@@ -335,16 +345,26 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     const Pair pair = find_pair(a, pick, pattern, nth);
     const uint64_t chose = __ballot(pair.at >= 0);
     if (!chose || (a.by_slot && __ballot(pair.at >= 0 && pair.at < nth))) return;
-    const int seg = pair.seg, n_all = __popcll(chose), groups = width_of(a, seg) / 16;
+    const int seg = pair.seg, n_all = __popcll(chose), groups = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)) / 16;
     if (pair.at >= 0) slots[wave][__popcll(chose & ((1ull << lane) - 1))] = (short)pair.at;      // each wave for itself
     const T *W1 = (const T *)a.W1 + (int64_t)seg * a.Fp * d, *b1 = a.b1 ? (const T *)a.b1 + (int64_t)seg * a.Fp : nullptr;
-    const int g0 = blockIdx.x % a.slices, r = (threadIdx.x >> 4) & 15, half = threadIdx.x >> 8, ch = threadIdx.x & 15;
-    typename Weights<T>::type w[STEPS];
+    // a round: G runs of channels, G 16 x 16 values over the waves' K; a thread stores up to two of them for one (token, slot)
+    const int g0 = blockIdx.x % a.slices * G, r = threadIdx.x & 15, ch0 = threadIdx.x >> 4;
+    constexpr int EACH = G == 1 ? 1 : G / 2;
+    typename Weights<T>::type w[G][STEPS];
+    float bias[EACH];
     auto fetch = [&](int g) {
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
-            const int k = (wave + j * WAVES) * 32 + kq;
-            w[j] = load8(W1 + (int64_t)(g * 16 + c) * d + k, g < groups && k < d);
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                const int k = (wave + j * WAVES) * 32 + kq;
+                w[i][j] = load8(W1 + (int64_t)((g + i) * 16 + c) * d + k, g + i < groups && k < d);
+            }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int ch = g * 16 + ch0 + i * 32;
+            bias[i] = b1 && ch < groups * 16 ? to_f32(b1[ch]) : 0.f;
         }
     };
     for (int t0 = 0; t0 < n_all; t0 += TILE_T) {
@@ -359,21 +379,34 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
         Operand<T> x[STEPS];
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) if (wave + j * WAVES < steps) x[j] = operand(row, wave + j * WAVES, std::integral_constant<int, 2>());
-        const int mine = half == 0 && r < n ? slots[wave][t0 + r] : -1;      // (token, slot) whose channel ch this thread stores
-        for (int g = g0, b = 0; g < groups; g += a.slices, b ^= 1) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        const int mine = r < n ? slots[wave][t0 + r] : -1;
+        for (int g = g0; g < groups; g += a.slices * G) {
+            f32x4 acc[G];
+            float bv[EACH];
 #pragma unroll
-            for (int j = 0; j < STEPS; ++j) if (wave + j * WAVES < steps) acc = x[j].template times<2>(w[j], acc);
-            fetch(g + a.slices);
+            for (int i = 0; i < G; ++i) {
+                acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part(wave, b * 16 + (lane >> 4) * 4 + e, c) = acc[e];
-            __syncthreads();                                 // two buffers: the next round's values go into the other one
-            if (mine >= 0) {
-                float z = 0.f;
+                for (int j = 0; j < STEPS; ++j) if (wave + j * WAVES < steps) acc[i] = x[j].template times<2>(w[i][j], acc[i]);
+            }
 #pragma unroll
-                for (int v = 0; v < WAVES; ++v) z += part(v, b * 16 + ch, r);
-                z = activated<T>(a.act, z + (b1 ? to_f32(b1[g * 16 + ch]) : 0.f));
-                const int64_t at = (int64_t)mine * a.Fp + g * 16 + ch;
+            for (int i = 0; i < EACH; ++i) bv[i] = bias[i];
+            fetch(g + a.slices * G);
+            if (g != g0) __syncthreads();                    // the last round's sums have been read
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part(wave, i * 16 + (lane >> 4) * 4 + e, c) = acc[i][e];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int at_ch = ch0 + i * 32, ch = g * 16 + at_ch;
+                if (mine < 0 || at_ch >= G * 16 || ch >= groups * 16) continue;
+                float z = bv[i];
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) z += part(v, at_ch, r);
+                z = activated<T>(a.act, z);
+                const int64_t at = (int64_t)mine * a.Fp + ch;
                 if constexpr (sizeof(T) == 2) {
                     const h16 hi = (h16)z;
                     ((h16 *)a.hid)[at] = hi;
@@ -388,21 +421,25 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 // Four features of all tokens.  A wave takes pairs in turn (or a range of a pair's channels) and multiplies in sixteen 4 x 4 blocks at once, four
 // features by four tokens, each over channels of its own: 16 bytes of a lane are eight channels of one feature.  The sums of the slots meet in LDS.
 template <class T>
-__global__ __launch_bounds__(NT) void moe_few_down_kernel(FewMoe a)
+__global__ __launch_bounds__(DOWN_WAVES * 64) void moe_few_down_kernel(FewMoe a)
 {
     extern __shared__ __attribute__((aligned(16))) float zs[];         // [parts][T k][4]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q4 = lane & 3, k8 = (lane >> 2) * 8;
     const int n0 = blockIdx.x * 4, d = a.d, all = a.T * a.top_k;
-    const int pattern = lane < a.T ? pattern_of(a, lane) : 0;
+    const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
     int pick[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) pick[s] = lane < a.T && s < a.top_k ? a.route[lane * a.top_k + s] : -1;
-    for (int item = wave; item < a.segs * a.parts; item += WAVES) {
+    // what the end needs: a thread's feature and token, at most 64 tokens x 4
+    const int f = threadIdx.x & 3, t = threadIdx.x >> 2;
+    const bool ends = t < a.T && n0 + f < d;
+    const float x = ends && a.add_residual ? to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]) : 0.f;
+    for (int item = wave; item < a.segs * a.parts; item += DOWN_WAVES) {
         const int nth = item / a.parts, prt = item - nth * a.parts;
         const Pair pair = find_pair(a, pick, pattern, nth);
         uint64_t chose = __ballot(pair.at >= 0);
         if (!chose || (a.by_slot && __ballot(pair.at >= 0 && pair.at < nth))) continue;
-        const int seg = pair.seg, width = width_of(a, seg), per = (width / 64 + a.parts - 1) / a.parts * 64;
+        const int seg = pair.seg, width = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)), per = (width / 64 + a.parts - 1) / a.parts * 64;
         const int from = prt * per, to = from + per < width ? from + per : width;
         const T *W = (const T *)a.W2T + ((int64_t)seg * d + (n0 + q4 < d ? n0 + q4 : d - 1)) * a.Fp + k8;
         while (chose) {                                      // up to sixteen tokens at a time
@@ -427,7 +464,7 @@ __global__ __launch_bounds__(NT) void moe_few_down_kernel(FewMoe a)
             f32x4 acc[TT];
 #pragma unroll
             for (int u = 0; u < TT; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            constexpr int AHEAD = 4;
+            constexpr int AHEAD = 8;
             for (int k = from; k < to; k += 128 * AHEAD) {
                 typename Weights<T>::type w[AHEAD];
 #pragma unroll
@@ -467,9 +504,7 @@ __global__ __launch_bounds__(NT) void moe_few_down_kernel(FewMoe a)
         }
     }
     __syncthreads();
-    const int f = threadIdx.x & 3, t = threadIdx.x >> 2;
-    if (t >= a.T || n0 + f >= d) return;
-    const float x = a.add_residual ? to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]) : 0.f;
+    if (!ends) return;
     const int p = pattern_of(a, t);
     float sum = 0.f;
     for (int s = 0; s < a.top_k; ++s) {
@@ -482,7 +517,7 @@ __global__ __launch_bounds__(NT) void moe_few_down_kernel(FewMoe a)
     ((T *)a.Y)[(int64_t)t * d + n0 + f] = from_f32<T>(x + sum);
 }
 
-struct FewWs { int32_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, parts; size_t bytes; };
+struct FewWs { int32_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, groups, parts; size_t bytes; };
 FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
 {
     Carver c(ws);
@@ -492,8 +527,10 @@ FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
     w.by_slot = pairs < D.P * m.n_experts;
     w.segs = w.by_slot ? pairs : D.P * m.n_experts;
     // a workgroup per compute unit: each routes for itself, so more of them would do that more often
-    w.slices = std::min(w.Fp / 16, std::max(1, 256 / w.segs));
-    w.parts = std::max(1, WAVES / w.segs);
+    w.slices = std::max(1, 256 / w.segs);
+    w.groups = w.Fp / 16 >= 4 * w.slices ? 4 : 1;
+    w.slices = std::min(ceil_div(w.Fp / 16, w.groups), w.slices);
+    w.parts = std::max(1, DOWN_WAVES / w.segs);
     w.route = c.take<int32_t>((size_t)pairs);
     w.weight = c.take<float>((size_t)pairs);
     w.hid = c.take<float>((size_t)pairs * w.Fp);
@@ -554,20 +591,20 @@ extern "C" int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_comp
     hipStream_t st = static_cast<hipStream_t>(stream);
     const size_t row = (align_up((size_t)D.d, 32) + 4) * sizeof(float);
     a.tile_rows = a.T * row <= XT_BYTES ? a.T : std::min(a.T, TILE_T);
-    const int red_e = std::max(32, (int)align_up((size_t)a.E, 16));
-    const size_t lds = a.tile_rows * row + ((size_t)WAVES * red_e * (TILE_T + 1) + (size_t)a.T * (a.E + 1)) * sizeof(float);
+    const size_t lds = a.tile_rows * row + ((size_t)WAVES * 64 * (TILE_T + 1) + (size_t)a.T * (a.E + 1)) * sizeof(float);
     const bool bf = D.dtype == SF_BF16;
-    auto kern = bf ? moe_few_up_kernel<h16> : moe_few_up_kernel<float>;
-    static std::atomic<bool> attr_set[2] = {{false}, {false}};      // setting the attribute twice is harmless
-    if (!attr_set[bf]) {
+    auto kern = w.groups == 4 ? (bf ? moe_few_up_kernel<h16, 4> : moe_few_up_kernel<float, 4>) : (bf ? moe_few_up_kernel<h16, 1> : moe_few_up_kernel<float, 1>);
+    static std::atomic<bool> attr_set[4];         // setting the attribute twice is harmless
+    const int which = bf + 2 * (w.groups == 4);
+    if (!attr_set[which]) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024) != hipSuccess)
             return fail(SF_ERR_HIP, "moe_ffn_few: cannot reserve LDS");
-        attr_set[bf] = true;
+        attr_set[which] = true;
     }
     hipLaunchKernelGGL(kern, dim3((unsigned)(w.segs * w.slices)), dim3(NT), lds, st, a);
     const dim3 down((unsigned)ceil_div(D.d, 4));
     const size_t zs = (size_t)w.parts * a.T * a.top_k * 4 * sizeof(float);
-    if (bf) hipLaunchKernelGGL(moe_few_down_kernel<h16>, down, dim3(NT), zs, st, a);
-    else hipLaunchKernelGGL(moe_few_down_kernel<float>, down, dim3(NT), zs, st, a);
+    if (bf) hipLaunchKernelGGL(moe_few_down_kernel<h16>, down, dim3(DOWN_WAVES * 64), zs, st, a);
+    else hipLaunchKernelGGL(moe_few_down_kernel<float>, down, dim3(DOWN_WAVES * 64), zs, st, a);
     return check_launch("moe_ffn_few_forward");
 }
