@@ -9,7 +9,6 @@
 // the logits, whose order decides.  fp32 models take the fp32 instruction.
 #include <algorithm>
 #include <atomic>
-#include <type_traits>
 
 #include "gemm.hpp"
 
@@ -36,7 +35,8 @@ struct FewMoe {
     int segs, by_slot, slices, parts;                        // pairs looked at (by_slot: those of each (token, slot), else all there are);
                                                              // workgroups of a pair (up), ranges of its channels (down)
     int tile_rows;                                           // normalised tokens in LDS at a time
-    int32_t *route; float *weight;                           // workspace: [T k] (-1: listed again in a later slot), [T k]
+    uint64_t *route; float *weight;                          // workspace, eight slots a token: experts in bytes (255: none, or listed again in a
+                                                             // later slot), weights
     void *hid;                                               // [T k, Fp] fp32, or the two terms [2, T k, Fp] in 16 bits
     void *Y; int32_t *route_out; float *weight_out, *logit_out;
 };
@@ -100,25 +100,32 @@ __device__ __forceinline__ int pattern_of(const FewMoe &a, int t)
 }
 
 // The `nth` pair looked at: its number (pattern E + expert), and the (token, slot) in which the lane's token chose it or -1.  by_slot: the pair of
-// (token, slot) nth, unless an earlier one is the same.  pick: the experts of the lane's token, negative where they do not count.  Registers of
-// one wave only.
+// (token, slot) nth.  picks: the experts of the lane's token, a byte each.  Registers of one wave only.
 struct Pair { int seg, at; };
-__device__ __forceinline__ Pair find_pair(const FewMoe &a, const int (&pick)[8], int pattern, int nth)
+__device__ __forceinline__ Pair find_pair(const FewMoe &a, uint64_t picks, int pattern, int nth)
 {
     const int lane = threadIdx.x & 63;
     Pair p{nth, -1};
     if (a.by_slot) {
         const int t = nth / a.top_k, s = nth - t * a.top_k;
-        int e = -1;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) e = q == s ? pick[q] : e;
-        e = __builtin_amdgcn_readlane(e, t);
-        p.seg = e < 0 ? -1 : __builtin_amdgcn_readlane(pattern, t) * a.E + e;
+        const uint64_t of = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(picks >> 32), t) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)picks, t);
+        const int e = (int)(of >> (8 * s)) & 255;
+        p.seg = e == 255 ? -1 : __builtin_amdgcn_readlane(pattern, t) * a.E + e;
     }
     if (p.seg < 0 || pattern != p.seg / a.E) return p;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) if (s < a.top_k && pick[s] == p.seg % a.E) p.at = lane * a.top_k + s;
+    const uint64_t x = picks ^ (uint64_t)(p.seg % a.E) * 0x0101010101010101ull;      // a zero byte where the expert is; E <= 64: none carries into the next
+    const uint64_t zero = ~((((x & 0x7f7f7f7f7f7f7f7full) + 0x7f7f7f7f7f7f7f7full) | x) | 0x7f7f7f7f7f7f7f7full);
+    if (zero) p.at = lane * a.top_k + (__ffsll((unsigned long long)zero) - 1) / 8;
     return p;
+}
+// The tokens that chose the pair: a list per wave, which that wave alone writes and reads.  0: not looked at here (none, or an earlier
+// (token, slot) is of the same pair)
+__device__ __forceinline__ int list_tokens(const FewMoe &a, const Pair &p, int nth, short *slots)
+{
+    const uint64_t chose = __ballot(p.at >= 0);
+    if (a.by_slot && __ballot(p.at >= 0 && p.at < nth)) return 0;
+    if (p.at >= 0) slots[__popcll(chose & ((1ull << (threadIdx.x & 63)) - 1))] = (short)p.at;
+    return __popcll(chose);
 }
 
 // Channels of an expert, padded as its weights are
@@ -128,30 +135,27 @@ __device__ __forceinline__ int width_of(const FewMoe &a, int kept)
     return w < a.Fp ? w : a.Fp;
 }
 
-// G: runs of sixteen channels per round of a workgroup, so that its weights are on their way together
+// One wave's 16 x 16 sums over its part of K are added up in LDS: [8 waves][64][17].
+//
+// A launch runs this code once, so its length counts: 35 KB of it, with every loop unrolled, took 24 500 clocks for one token of eight experts, of which
+// the choice of two experts alone was 5700; what is not a load ahead of its use is a loop here.
+// G: runs of sixteen channels per round of a workgroup, so that its weights are on their way together.
 template <class T, int G>
 __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 {
-    // [tile_rows][dp + 4] normalised tokens (rows 16 bytes apart over the banks), then partial sums [8][64][17], then logits [T][E + 1]
+    // [tile_rows][dp + 4] normalised tokens (rows 16 bytes apart over the banks), then partial sums, then logits [T][E + 1]
     extern __shared__ __attribute__((aligned(16))) float xt[];
     __shared__ float mean[FEW], rstd[FEW];
+    __shared__ uint64_t picks[FEW];
     __shared__ short slots[WAVES][FEW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kq = (lane >> 4) * 8;
-    const int d = a.d, dp = (d + 31) / 32 * 32, ld = dp + 4, steps = dp / 32, lgs = a.E + 1, tiles_e = (a.E + 15) / 16;
+    const int d = a.d, dp = (d + 31) / 32 * 32, ld = dp + 4, steps = dp / 32, lgs = a.E + 1;
     float *red = xt + a.tile_rows * ld, *lg = red + WAVES * 64 * (TILE_T + 1);
     auto part = [&](int w, int e, int r) -> float & { return red[(w * 64 + e) * (TILE_T + 1) + r]; };
-    // what does not depend on the tokens is on its way first
-    const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
-    const float bias_r = a.br && lane < a.E ? to_f32(((const T *)a.br)[lane]) : 0.f;
-    typename Weights<T>::type wr[STEPS];
-#pragma unroll
-    for (int j = 0; j < STEPS; ++j) wr[j] = load8((const T *)a.Wr + (int64_t)c * d + (wave + j * WAVES) * 32 + kq, c < a.E && (wave + j * WAVES) * 32 + kq < d);
     const T *X = (const T *)a.X;
     constexpr int NCH = MAX_D / 512;
-    float gm[NCH][8], bt[NCH][8];
-    auto eight = [&](const T *p, int j, float *v) {
-        const int at = (lane + j * 64) * 8;
-        const auto q = load8(p + at, at < d);
+    typedef typename Weights<T>::type Eight;
+    auto to_floats = [](const Eight &q, float *v) {
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = (float)q[e];
@@ -160,198 +164,167 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
             for (int e = 0; e < 4; ++e) { v[e] = q.a[e]; v[4 + e] = q.b[e]; }
         }
     };
-    if (a.ln_g) {
+    // what does not depend on the tokens is on its way first
+    const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
+    const float bias_r = a.br && lane < a.E ? to_f32(((const T *)a.br)[lane]) : 0.f;
+    Eight gq[NCH], bq[NCH], wr[STEPS];
 #pragma unroll
-        for (int j = 0; j < NCH; ++j) { eight((const T *)a.ln_g, j, gm[j]); eight((const T *)a.ln_b, j, bt[j]); }
+    for (int j = 0; j < NCH; ++j) {
+        const int at = (lane + j * 64) * 8;
+        gq[j] = load8((const T *)a.ln_g + at, a.ln_g && at < d);
+        bq[j] = load8((const T *)a.ln_b + at, a.ln_g && at < d);
     }
-    // tokens of(0) .. of(n - 1) normalised into rows r0 .. of xt; statistics the first time.  A wave takes two of them at once.
-    auto normalise = [&](int n, int r0, bool first, auto of) {
-        for (int i = wave; i < n; i += 2 * WAVES) {
-            float v[2][NCH][8];
-            int t[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int k = i + u * WAVES;
-                t[u] = of(k < n ? k : i);
-#pragma unroll
-                for (int j = 0; j < NCH; ++j) eight(X + (int64_t)t[u] * d, j, v[u][j]);
-            }
-            if (a.ln_g) {
-                float m[2], inv[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    if (first) {
-                        float sum = 0.f, q = 0.f;
-#pragma unroll
-                        for (int j = 0; j < NCH; ++j)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) sum += v[u][j][e];
-                        m[u] = wave_sum(sum) / d;
-#pragma unroll
-                        for (int j = 0; j < NCH; ++j)
-                            if ((lane + j * 64) * 8 < d) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) q = fmaf(v[u][j][e] - m[u], v[u][j][e] - m[u], q);
-                            }
-                        inv[u] = 1.0f / sqrtf(wave_sum(q) / d + a.eps);
-                        if (lane == 0) { mean[t[u]] = m[u]; rstd[t[u]] = inv[u]; }
-                    } else { m[u] = mean[t[u]]; inv[u] = rstd[t[u]]; }
-#pragma unroll
-                    for (int j = 0; j < NCH; ++j)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[u][j][e] = fmaf((v[u][j][e] - m[u]) * inv[u], gm[j][e], bt[j][e]);
-                }
-            }
+    for (int j = 0; j < STEPS; ++j) wr[j] = load8((const T *)a.Wr + (int64_t)c * d + (wave + j * WAVES) * 32 + kq, c < a.E && (wave + j * WAVES) * 32 + kq < d);
+
+    // ---- route
+    const bool resident = a.T <= a.tile_rows;
+    for (int base = 0; base < a.T; base += a.tile_rows) {
+        const int rows = a.T - base < a.tile_rows ? a.T - base : a.tile_rows;
+        // two tokens of a wave at a time
+        for (int i = wave; i < rows; i += 2 * WAVES) {
+            Eight xq[2][NCH];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int j = 0; j < NCH; ++j) {
                     const int at = (lane + j * 64) * 8;
-                    if (i + u * WAVES >= n || at >= dp) continue;
-                    float *o = xt + (r0 + i + u * WAVES) * ld + at;
-                    const bool in = at < d;                  // zeros from d to the next multiple of 32
+                    xq[u][j] = load8(X + (int64_t)(base + i + u * WAVES) * d + at, at < d && i + u * WAVES < rows);
+                }
+            float v[2][NCH][8], m[2], inv[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                m[u] = 0.f;
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) {
+                    to_floats(xq[u][j], v[u][j]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) m[u] += v[u][j][e];
+                }
+            }
+            if (a.ln_g) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    m[u] = wave_sum(m[u]) / d;
+                    inv[u] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NCH; ++j)
+                        if ((lane + j * 64) * 8 < d) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) inv[u] = fmaf(v[u][j][e] - m[u], v[u][j][e] - m[u], inv[u]);
+                        }
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) inv[u] = 1.0f / sqrtf(wave_sum(inv[u]) / d + a.eps);
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) {
+                    float gm[8], bt[8];
+                    to_floats(gq[j], gm);
+                    to_floats(bq[j], bt);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][j][e] = fmaf((v[u][j][e] - m[u]) * inv[u], gm[e], bt[e]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int r = i + u * WAVES;
+                if (r >= rows) break;
+                if (lane == 0 && a.ln_g) { mean[base + r] = m[u]; rstd[base + r] = inv[u]; }
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) {
+                    const int at = (lane + j * 64) * 8;
+                    if (at >= dp) continue;                  // zeros from d to the next multiple of 32
+                    float *o = xt + r * ld + at;
+                    const bool in = at < d;
                     *reinterpret_cast<f32x4 *>(o) = in ? f32x4{v[u][j][0], v[u][j][1], v[u][j][2], v[u][j][3]} : f32x4{0.f, 0.f, 0.f, 0.f};
                     *reinterpret_cast<f32x4 *>(o + 4) = in ? f32x4{v[u][j][4], v[u][j][5], v[u][j][6], v[u][j][7]} : f32x4{0.f, 0.f, 0.f, 0.f};
                 }
+            }
         }
-    };
-    // K step s of row r of xt, as TERMS terms
-    auto operand = [&](int r, int s, auto terms) {
-        float v[8];
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        const float *p = xt + r * ld + s * 32 + kq;
-        const f32x4 lo = r >= 0 ? *reinterpret_cast<const f32x4 *>(p) : zero, hi = r >= 0 ? *reinterpret_cast<const f32x4 *>(p + 4) : zero;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
-        return Operand<T>::template split<decltype(terms)::value>(v);
-    };
-
-    // ---- route
-    const bool resident = a.T <= a.tile_rows;
-    if (resident) {
-        normalise(a.T, 0, true, [](int i) { return i; });
         __syncthreads();
-    }
-    for (int t0 = 0; t0 < a.T; t0 += TILE_T) {
-        const int n = a.T - t0 < TILE_T ? a.T - t0 : TILE_T;
-        if (!resident) {
-            normalise(n, 0, true, [&](int i) { return t0 + i; });
+        for (int t0 = 0; t0 < rows; t0 += TILE_T) {
+            const int n = rows - t0 < TILE_T ? rows - t0 : TILE_T;
+            for (int e0 = 0; e0 < a.E; e0 += 16) {
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < STEPS; ++j) {
+                    const int s = wave + j * WAVES;
+                    if (s >= steps) break;
+                    Eight w = wr[j];
+                    if (e0) w = load8((const T *)a.Wr + (int64_t)(e0 + c) * d + s * 32 + kq, e0 + c < a.E && s * 32 + kq < d);
+                    float v[8];
+                    const float *p = xt + (t0 + (c < n ? c : 0)) * ld + s * 32 + kq;      // columns from n on: another's sums, not stored
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = p[e];
+                    acc = Operand<T>::template split<3>(v).template times<3>(w, acc);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part(wave, e0 + (lane >> 4) * 4 + e, c) = acc[e];
+            }
+            __syncthreads();
+            // a wave per token, a lane per expert.  An expert's rank is the number of those before it: higher logits, and equal ones of lower
+            // numbers; a NaN ranks below every number.  An expert that the caller lists twice counts in its last slot.
+            for (int r = wave; r < n; r += WAVES) {
+                const int t = base + t0 + r;
+                float sum = bias_r;
+                if (lane < a.E) {
+                    float q = 0.f;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) q += part(w, lane, r);
+                    sum += q;
+                    lg[t * lgs + lane] = sum;
+                }
+                float mine = lane < a.E && sum == sum ? sum : -INFINITY;
+                int slot, expert = lane;
+                if (a.forced) {
+                    expert = lane < a.top_k ? min(max(a.forced[t * a.top_k + lane], 0), a.E - 1) : -1;
+                    mine = __int_as_float(__builtin_amdgcn_ds_bpermute(4 * max(expert, 0), __float_as_int(mine)));
+                    slot = lane < a.top_k ? lane : 8;
+                    for (int q = 0; q < a.top_k; ++q)
+                        if (q > lane && __builtin_amdgcn_readlane(expert, q) == expert) mine = -INFINITY, slot = 9 + lane;      // again, later
+                } else {
+                    slot = 0;
+                    for (int e = 0; e < a.E; ++e) {
+                        const float u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), e));
+                        slot += u > mine || (u == mine && e < lane);
+                    }
+                    slot = lane < a.E && slot < a.top_k ? slot : 8;
+                }
+                const bool in = slot < 8, listed = in || slot > 8;
+                float most = in ? mine : -INFINITY;
+#pragma unroll 1
+                for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+                const float ex = in ? expf(mine - most) : 0.f, w = ex / wave_sum(ex);
+                uint8_t *pk = reinterpret_cast<uint8_t *>(&picks[t]);
+                if (lane < 8) pk[lane] = 255;
+                if (in) pk[slot] = (uint8_t)expert;
+                if (blockIdx.x == 0 && listed) {
+                    const int s = in ? slot : slot - 9;
+                    a.weight[t * 8 + s] = w;
+                    if (a.route_out) a.route_out[t * a.top_k + s] = expert;
+                    if (a.weight_out) a.weight_out[t * a.top_k + s] = w;
+                }
+                if (blockIdx.x == 0 && a.logit_out && lane < a.E) a.logit_out[t * a.E + lane] = sum;
+            }
             __syncthreads();
         }
-        f32x4 acc[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
-            const int s = wave + j * WAVES;
-            if (s >= steps) break;
-            typename Weights<T>::type w[4];
-            w[0] = wr[j];
-#pragma unroll
-            for (int i = 1; i < 4; ++i) {
-                const int e = i * 16 + c;
-                if (i < tiles_e) w[i] = load8((const T *)a.Wr + (int64_t)e * d + s * 32 + kq, e < a.E && s * 32 + kq < d);
-            }
-            const auto x = operand(c < n ? (resident ? t0 + c : c) : -1, s, std::integral_constant<int, 3>());
-#pragma unroll
-            for (int i = 0; i < 4; ++i) if (i < tiles_e) acc[i] = x.template times<3>(w[i], acc[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i >= tiles_e) break;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) part(wave, i * 16 + (lane >> 4) * 4 + e, c) = acc[i][e];
-        }
-        __syncthreads();
-        for (int r = wave; r < n; r += WAVES)                // a lane per expert
-            if (lane < a.E) {
-                float sum = 0.f;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) sum += part(w, lane, r);
-                lg[(t0 + r) * lgs + lane] = sum + bias_r;
-            }
-        __syncthreads();
     }
-    // Every wave chooses for all tokens, a lane each.  Ties go to the lower expert, a NaN ranks below every number; an expert that the caller
-    // lists twice counts in its last slot.
-    const bool one = blockIdx.x == 0;
-    int pick[8];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) pick[s] = -1;
-    if (lane < a.T) {
-        const int t = lane;
-        const float *my = lg + t * lgs;
-        unsigned long long taken = 0;
-        float most = -INFINITY, den = 0.f, v[8];
-        int who[8];
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            who[s] = -1;
-            v[s] = -INFINITY;
-            if (s >= a.top_k) continue;
-            int be = -1;
-            float bv = -INFINITY;
-            if (a.forced) {
-                be = min(max(a.forced[t * a.top_k + s], 0), a.E - 1);
-                bv = my[be];
-                bv = bv == bv ? bv : -INFINITY;
-            } else {
-                for (int e0 = 0; e0 < a.E; e0 += 8) {
-                    float u[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = my[e0 + e < a.E ? e0 + e : 0];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = u[e] == u[e] ? u[e] : -INFINITY;
-                        if (e0 + e < a.E && !(taken >> (e0 + e) & 1) && (be < 0 || x > bv)) { be = e0 + e; bv = x; }
-                    }
-                }
-                taken |= 1ull << be;
-            }
-            who[s] = be;
-            v[s] = bv;
-        }
-        bool again[8];
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            again[s] = false;
-#pragma unroll
-            for (int q = s + 1; q < 8; ++q) again[s] = again[s] || (q < a.top_k && who[q] == who[s]);
-            if (!again[s]) most = fmaxf(most, v[s]);
-            pick[s] = again[s] ? -1 : who[s];
-        }
-        if (one && wave == 0) {
-#pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                v[s] = s < a.top_k && !again[s] ? expf(v[s] - most) : 0.f;
-                den += v[s];
-            }
-#pragma unroll
-            for (int s = 0; s < 8; ++s) {
-                if (s >= a.top_k) continue;
-                const int i = t * a.top_k + s;
-                a.route[i] = pick[s];
-                a.weight[i] = v[s] / den;
-                if (a.route_out) a.route_out[i] = who[s];
-                if (a.weight_out) a.weight_out[i] = v[s] / den;
-            }
-        }
-    }
-    if (one && a.logit_out)
-        for (int i = threadIdx.x; i < a.T * a.E; i += NT) a.logit_out[i] = lg[i / a.E * lgs + i % a.E];
+    const uint64_t mine_picks = lane < a.T ? picks[lane] : ~0ull;
+    if (blockIdx.x == 0 && threadIdx.x < a.T) a.route[threadIdx.x] = mine_picks;
 
     // ---- channels of a pair
     const int nth = blockIdx.x / a.slices;
-    const Pair pair = find_pair(a, pick, pattern, nth);
-    const uint64_t chose = __ballot(pair.at >= 0);
-    if (!chose || (a.by_slot && __ballot(pair.at >= 0 && pair.at < nth))) return;
-    const int seg = pair.seg, n_all = __popcll(chose), groups = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)) / 16;
-    if (pair.at >= 0) slots[wave][__popcll(chose & ((1ull << lane) - 1))] = (short)pair.at;      // each wave for itself
+    const Pair pair = find_pair(a, mine_picks, pattern, nth);
+    const int n_all = list_tokens(a, pair, nth, slots[wave]);
+    if (!n_all) return;
+    const int seg = pair.seg, groups = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)) / 16;
     const T *W1 = (const T *)a.W1 + (int64_t)seg * a.Fp * d, *b1 = a.b1 ? (const T *)a.b1 + (int64_t)seg * a.Fp : nullptr;
     // a round: G runs of channels, G 16 x 16 values over the waves' K; a thread stores up to two of them for one (token, slot)
     const int g0 = blockIdx.x % a.slices * G, r = threadIdx.x & 15, ch0 = threadIdx.x >> 4;
     constexpr int EACH = G == 1 ? 1 : G / 2;
-    typename Weights<T>::type w[G][STEPS];
+    Eight w[G][STEPS];
     float bias[EACH];
     auto fetch = [&](int g) {
 #pragma unroll
@@ -370,15 +343,28 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     for (int t0 = 0; t0 < n_all; t0 += TILE_T) {
         fetch(g0);
         const int n = n_all - t0 < TILE_T ? n_all - t0 : TILE_T;
-        if (!resident) {
-            __syncthreads();
-            normalise(n, 0, false, [&](int i) { return slots[wave][t0 + i] / a.top_k; });
-        }
-        __syncthreads();
-        const int row = c < n ? (resident ? slots[wave][t0 + c] / a.top_k : c) : -1;
+        const int token = slots[wave][t0 + (c < n ? c : 0)] / a.top_k;        // columns from n on: another's sums, not stored
         Operand<T> x[STEPS];
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j) if (wave + j * WAVES < steps) x[j] = operand(row, wave + j * WAVES, std::integral_constant<int, 2>());
+        for (int j = 0; j < STEPS; ++j) {
+            const int k = (wave + j * WAVES) * 32 + kq;
+            if (wave + j * WAVES >= steps) break;
+            float v[8];
+            if (resident) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = xt[token * ld + k + e];
+            } else {                                         // normalised again, from memory
+                to_floats(load8(X + (int64_t)token * d + k, k < d), v);
+                if (a.ln_g) {
+                    float gm[8], bt[8];
+                    to_floats(load8((const T *)a.ln_g + k, k < d), gm);
+                    to_floats(load8((const T *)a.ln_b + k, k < d), bt);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf((v[e] - mean[token]) * rstd[token], gm[e], bt[e]);
+                }
+            }
+            x[j] = Operand<T>::template split<2>(v);
+        }
         const int mine = r < n ? slots[wave][t0 + r] : -1;
         for (int g = g0; g < groups; g += a.slices * G) {
             f32x4 acc[G];
@@ -392,7 +378,7 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 #pragma unroll
             for (int i = 0; i < EACH; ++i) bv[i] = bias[i];
             fetch(g + a.slices * G);
-            if (g != g0) __syncthreads();                    // the last round's sums have been read
+            __syncthreads();                                 // the last round's sums have been read
 #pragma unroll
             for (int i = 0; i < G; ++i)
 #pragma unroll
@@ -414,7 +400,6 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
                 } else ((float *)a.hid)[at] = z;
             }
         }
-        __syncthreads();
     }
 }
 
@@ -424,54 +409,51 @@ template <class T>
 __global__ __launch_bounds__(DOWN_WAVES * 64) void moe_few_down_kernel(FewMoe a)
 {
     extern __shared__ __attribute__((aligned(16))) float zs[];         // [parts][T k][4]
+    __shared__ short slots[DOWN_WAVES][FEW + 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q4 = lane & 3, k8 = (lane >> 2) * 8;
     const int n0 = blockIdx.x * 4, d = a.d, all = a.T * a.top_k;
+    const uint64_t picks = lane < a.T ? a.route[lane] : ~0ull;
     const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
-    int pick[8];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) pick[s] = lane < a.T && s < a.top_k ? a.route[lane * a.top_k + s] : -1;
     // what the end needs: a thread's feature and token, at most 64 tokens x 4
     const int f = threadIdx.x & 3, t = threadIdx.x >> 2;
     const bool ends = t < a.T && n0 + f < d;
-    const float x = ends && a.add_residual ? to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]) : 0.f;
+    float y = 0.f;
+    f32x4 wt[2] = {};
+    uint64_t slot_of = ~0ull;
+    if (ends) {
+        if (a.add_residual) y = to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]);
+        wt[0] = *reinterpret_cast<const f32x4 *>(a.weight + t * 8);
+        wt[1] = *reinterpret_cast<const f32x4 *>(a.weight + t * 8 + 4);
+        slot_of = a.route[t];
+    }
     for (int item = wave; item < a.segs * a.parts; item += DOWN_WAVES) {
         const int nth = item / a.parts, prt = item - nth * a.parts;
-        const Pair pair = find_pair(a, pick, pattern, nth);
-        uint64_t chose = __ballot(pair.at >= 0);
-        if (!chose || (a.by_slot && __ballot(pair.at >= 0 && pair.at < nth))) continue;
+        const Pair pair = find_pair(a, picks, pattern, nth);
+        const int n_all = list_tokens(a, pair, nth, slots[wave]);
+        if (!n_all) continue;
         const int seg = pair.seg, width = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)), per = (width / 64 + a.parts - 1) / a.parts * 64;
         const int from = prt * per, to = from + per < width ? from + per : width;
         const T *W = (const T *)a.W2T + ((int64_t)seg * d + (n0 + q4 < d ? n0 + q4 : d - 1)) * a.Fp + k8;
-        while (chose) {                                      // up to sixteen tokens at a time
-            constexpr int TT = 4;
-            int at[TT], n = 0;
+        f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+        if (a.b2x && prt == 0) {
 #pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                // the lane's token of the next four
-                uint64_t four = chose;
-                at[u] = -1;
+            for (int e = 0; e < 4; ++e) bias[e] = to_f32(((const T *)a.b2x)[(int64_t)seg * d + (n0 + e < d ? n0 + e : d - 1)]);
+        }
+        for (int t0 = 0; t0 < n_all; t0 += 16) {             // up to sixteen tokens at a time, four to a product
+            constexpr int TT = 4, AHEAD = 8;
+            int at[TT];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    if (!four) break;
-                    const int t = __ffsll((unsigned long long)four) - 1;
-                    four &= four - 1;
-                    const int s = __builtin_amdgcn_readlane(pair.at, t);
-                    if (q4 == v) at[u] = s;
-                    ++n;
-                }
-                chose = four;
-            }
+            for (int u = 0; u < TT; ++u) at[u] = t0 + u * 4 + q4 < n_all ? slots[wave][t0 + u * 4 + q4] : -1;
             f32x4 acc[TT];
 #pragma unroll
             for (int u = 0; u < TT; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            constexpr int AHEAD = 8;
             for (int k = from; k < to; k += 128 * AHEAD) {
                 typename Weights<T>::type w[AHEAD];
 #pragma unroll
                 for (int j = 0; j < AHEAD; ++j) w[j] = load8(W + k + j * 128, k + j * 128 + k8 < to);
 #pragma unroll
                 for (int u = 0; u < TT; ++u) {
-                    if (u * 4 >= n) break;
+                    if (t0 + u * 4 >= n_all) break;
 #pragma unroll
                     for (int j = 0; j < AHEAD; ++j) {
                         const bool in = at[u] >= 0 && k + j * 128 + k8 < to;
@@ -496,28 +478,28 @@ __global__ __launch_bounds__(DOWN_WAVES * 64) void moe_few_down_kernel(FewMoe a)
             }
 #pragma unroll
             for (int u = 0; u < TT; ++u) {
-                if (u * 4 >= n) break;
+                if (t0 + u * 4 >= n_all) break;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[u][e] = pair_sum<4>(pair_sum<8>(pair_sum<16>(pair_sum<32>(acc[u][e]))));
+                for (int e = 0; e < 4; ++e) acc[u][e] = pair_sum<4>(pair_sum<8>(pair_sum<16>(pair_sum<32>(acc[u][e])))) + bias[e];
                 if (lane < 4 && at[u] >= 0) *reinterpret_cast<f32x4 *>(zs + (prt * all + at[u]) * 4) = acc[u];
             }
         }
     }
     __syncthreads();
     if (!ends) return;
-    const int p = pattern_of(a, t);
     float sum = 0.f;
-    for (int s = 0; s < a.top_k; ++s) {
-        const int i = t * a.top_k + s, e = a.route[i];
-        if (e < 0) continue;
-        float z = a.b2x ? to_f32(((const T *)a.b2x)[((int64_t)p * a.E + e) * d + n0 + f]) : 0.f;
-        for (int q = 0; q < a.parts; ++q) z += zs[(q * all + i) * 4 + f];
-        sum = fmaf(a.weight[i], z, sum);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+        if (s >= a.top_k) break;
+        if (((slot_of >> (8 * s)) & 255) == 255) continue;
+        float z = 0.f;
+        for (int q = 0; q < a.parts; ++q) z += zs[(q * all + t * a.top_k + s) * 4 + f];
+        sum = fmaf(wt[s / 4][s % 4], z, sum);
     }
-    ((T *)a.Y)[(int64_t)t * d + n0 + f] = from_f32<T>(x + sum);
+    ((T *)a.Y)[(int64_t)t * d + n0 + f] = from_f32<T>(y + sum);
 }
 
-struct FewWs { int32_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, groups, parts; size_t bytes; };
+struct FewWs { uint64_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, groups, parts; size_t bytes; };
 FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
 {
     Carver c(ws);
@@ -531,8 +513,8 @@ FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
     w.groups = w.Fp / 16 >= 4 * w.slices ? 4 : 1;
     w.slices = std::min(ceil_div(w.Fp / 16, w.groups), w.slices);
     w.parts = std::max(1, DOWN_WAVES / w.segs);
-    w.route = c.take<int32_t>((size_t)pairs);
-    w.weight = c.take<float>((size_t)pairs);
+    w.route = c.take<uint64_t>((size_t)T);
+    w.weight = c.take<float>((size_t)T * 8);
     w.hid = c.take<float>((size_t)pairs * w.Fp);
     w.bytes = c.off;
     return w;
