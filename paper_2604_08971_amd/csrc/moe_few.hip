@@ -166,7 +166,6 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     };
     // what does not depend on the tokens is on its way first
     const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
-    const float bias_r = a.br && lane < a.E ? to_f32(((const T *)a.br)[lane]) : 0.f;
     Eight gq[NCH], bq[NCH], wr[STEPS];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
@@ -181,16 +180,25 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     const bool resident = a.T <= a.tile_rows;
     for (int base = 0; base < a.T; base += a.tile_rows) {
         const int rows = a.T - base < a.tile_rows ? a.T - base : a.tile_rows;
-        // two tokens of a wave at a time
-        for (int i = wave; i < rows; i += 2 * WAVES) {
-            Eight xq[2][NCH];
+        // two tokens of a wave at a time, the next two on their way
+        Eight next[2][NCH];
+        auto load_tokens = [&](int i) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int j = 0; j < NCH; ++j) {
                     const int at = (lane + j * 64) * 8;
-                    xq[u][j] = load8(X + (int64_t)(base + i + u * WAVES) * d + at, at < d && i + u * WAVES < rows);
+                    next[u][j] = load8(X + (int64_t)(base + i + u * WAVES) * d + at, at < d && i + u * WAVES < rows);
                 }
+        };
+        load_tokens(wave);
+        for (int i = wave; i < rows; i += 2 * WAVES) {
+            Eight xq[2][NCH];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) xq[u][j] = next[u][j];
+            load_tokens(i + 2 * WAVES);
             float v[2][NCH][8], m[2], inv[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -244,9 +252,12 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
             }
         }
         __syncthreads();
-        for (int t0 = 0; t0 < rows; t0 += TILE_T) {
-            const int n = rows - t0 < TILE_T ? rows - t0 : TILE_T;
-            for (int e0 = 0; e0 < a.E; e0 += 16) {
+        // logits in blocks of 16 experts x 16 tokens, four blocks between two barriers
+        const int tiles_e = (a.E + 15) / 16, blocks = tiles_e * ((rows + TILE_T - 1) / TILE_T);
+        for (int b0 = 0; b0 < blocks; b0 += 4) {
+            const int nb = blocks - b0 < 4 ? blocks - b0 : 4;
+            for (int i = 0; i < nb; ++i) {
+                const int e0 = (b0 + i) % tiles_e * 16, r = (b0 + i) / tiles_e * TILE_T + c;
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < STEPS; ++j) {
@@ -255,64 +266,70 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
                     Eight w = wr[j];
                     if (e0) w = load8((const T *)a.Wr + (int64_t)(e0 + c) * d + s * 32 + kq, e0 + c < a.E && s * 32 + kq < d);
                     float v[8];
-                    const float *p = xt + (t0 + (c < n ? c : 0)) * ld + s * 32 + kq;      // columns from n on: another's sums, not stored
+                    const float *p = xt + (r < rows ? r : 0) * ld + s * 32 + kq;      // columns from `rows` on: another's sums, not stored
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = p[e];
                     acc = Operand<T>::template split<3>(v).template times<3>(w, acc);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) part(wave, e0 + (lane >> 4) * 4 + e, c) = acc[e];
+                for (int e = 0; e < 4; ++e) part(wave, i * 16 + (lane >> 4) * 4 + e, c) = acc[e];
             }
             __syncthreads();
-            // a wave per token, a lane per expert.  An expert's rank is the number of those before it: higher logits, and equal ones of lower
-            // numbers; a NaN ranks below every number.  An expert that the caller lists twice counts in its last slot.
-            for (int r = wave; r < n; r += WAVES) {
-                const int t = base + t0 + r;
-                float sum = bias_r;
-                if (lane < a.E) {
-                    float q = 0.f;
+            for (int i = threadIdx.x; i < nb * 256; i += NT) {
+                const int e = (b0 + i / 256) % tiles_e * 16 + (i >> 4) % 16, r = (b0 + i / 256) / tiles_e * TILE_T + (i & 15);
+                if (e >= a.E || r >= rows) continue;
+                float q = 0.f;
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) q += part(w, lane, r);
-                    sum += q;
-                    lg[t * lgs + lane] = sum;
-                }
-                float mine = lane < a.E && sum == sum ? sum : -INFINITY;
-                int slot, expert = lane;
-                if (a.forced) {
-                    expert = lane < a.top_k ? min(max(a.forced[t * a.top_k + lane], 0), a.E - 1) : -1;
-                    mine = __int_as_float(__builtin_amdgcn_ds_bpermute(4 * max(expert, 0), __float_as_int(mine)));
-                    slot = lane < a.top_k ? lane : 8;
-                    for (int q = 0; q < a.top_k; ++q)
-                        if (q > lane && __builtin_amdgcn_readlane(expert, q) == expert) mine = -INFINITY, slot = 9 + lane;      // again, later
-                } else {
-                    slot = 0;
-                    for (int e = 0; e < a.E; ++e) {
-                        const float u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), e));
-                        slot += u > mine || (u == mine && e < lane);
-                    }
-                    slot = lane < a.E && slot < a.top_k ? slot : 8;
-                }
-                const bool in = slot < 8, listed = in || slot > 8;
-                float most = in ? mine : -INFINITY;
-#pragma unroll 1
-                for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-                const float ex = in ? expf(mine - most) : 0.f, w = ex / wave_sum(ex);
-                uint8_t *pk = reinterpret_cast<uint8_t *>(&picks[t]);
-                if (lane < 8) pk[lane] = 255;
-                if (in) pk[slot] = (uint8_t)expert;
-                if (blockIdx.x == 0 && listed) {
-                    const int s = in ? slot : slot - 9;
-                    a.weight[t * 8 + s] = w;
-                    if (a.route_out) a.route_out[t * a.top_k + s] = expert;
-                    if (a.weight_out) a.weight_out[t * a.top_k + s] = w;
-                }
-                if (blockIdx.x == 0 && a.logit_out && lane < a.E) a.logit_out[t * a.E + lane] = sum;
+                for (int w = 0; w < WAVES; ++w) q += part(w, i >> 4, i & 15);
+                lg[(base + r) * lgs + e] = q + (a.br ? to_f32(((const T *)a.br)[e]) : 0.f);
             }
             __syncthreads();
         }
     }
+    // An expert's rank is the number of those before it: higher logits, and equal ones of lower numbers; a NaN ranks below every number.  An
+    // expert that the caller lists twice counts in its last slot.
+    uint8_t *pk = reinterpret_cast<uint8_t *>(picks);
+    for (int i = threadIdx.x; i < a.T * 8; i += NT) if (i % 8 >= a.top_k) pk[i] = 255;
+    if (a.forced) {
+        for (int i = threadIdx.x; i < a.T * a.top_k; i += NT) {
+            const int t = i / a.top_k, s = i - t * a.top_k, e = min(max(a.forced[i], 0), a.E - 1);
+            bool again = false;
+            for (int q = s + 1; q < a.top_k; ++q) again = again || min(max(a.forced[t * a.top_k + q], 0), a.E - 1) == e;
+            pk[t * 8 + s] = again ? 255 : (uint8_t)e;
+        }
+    } else {
+        for (int i = threadIdx.x; i < a.T * a.E; i += NT) {
+            const int t = i / a.E, e = i - t * a.E;
+            const float *l = lg + t * lgs;
+            const float mine = l[e] == l[e] ? l[e] : -INFINITY;
+            int rank = 0;
+#pragma unroll 8
+            for (int q = 0; q < a.E; ++q) {
+                const float u = l[q] == l[q] ? l[q] : -INFINITY;
+                rank += u > mine || (u == mine && q < e);
+            }
+            if (rank < a.top_k) pk[t * 8 + rank] = (uint8_t)e;
+        }
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) {
+        if (a.logit_out) for (int i = threadIdx.x; i < a.T * a.E; i += NT) a.logit_out[i] = lg[i / a.E * lgs + i % a.E];
+        if (threadIdx.x < a.T) {
+            const int t = threadIdx.x;
+            float most = -INFINITY, den = 0.f;
+            auto logit = [&](int s) { const int e = pk[t * 8 + s]; return e == 255 || !(lg[t * lgs + e] == lg[t * lgs + e]) ? -INFINITY : lg[t * lgs + e]; };
+            for (int s = 0; s < a.top_k; ++s) most = fmaxf(most, logit(s));
+            for (int s = 0; s < a.top_k; ++s) den += pk[t * 8 + s] == 255 ? 0.f : expf(logit(s) - most);
+            for (int s = 0; s < a.top_k; ++s) {
+                const float w = pk[t * 8 + s] == 255 ? 0.f : expf(logit(s) - most) / den;
+                a.weight[t * 8 + s] = w;
+                if (a.weight_out) a.weight_out[t * a.top_k + s] = w;
+                if (a.route_out) a.route_out[t * a.top_k + s] = a.forced ? min(max(a.forced[t * a.top_k + s], 0), a.E - 1) : pk[t * 8 + s];
+            }
+            a.route[t] = picks[t];
+        }
+    }
     const uint64_t mine_picks = lane < a.T ? picks[lane] : ~0ull;
-    if (blockIdx.x == 0 && threadIdx.x < a.T) a.route[threadIdx.x] = mine_picks;
 
     // ---- channels of a pair
     const int nth = blockIdx.x / a.slices;
