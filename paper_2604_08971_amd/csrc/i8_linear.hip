@@ -199,7 +199,7 @@ FfnI8Ws ffn_ws(const Dims &D, int Fp, void *ws)
     w.sx = c.take<float>(rows);
     w.hq = c.take<int8_t>(rows * Fp);
     w.sh = c.take<float>(rows);
-    w.part = c.take<float>(rows * ceil_div(Fp, 128));
+    w.part = c.take<float>(rows * ceil_div(Fp, 64));
     w.hid = ffn_few(D, Fp) ? c.take<float>(rows * Fp) : nullptr;
     w.bytes = c.off;
     return w;

@@ -457,7 +457,7 @@ __global__ __launch_bounds__(DOWN_WAVES * 64) void moe_few_down_kernel(FewMoe a)
             for (int e = 0; e < 4; ++e) bias[e] = to_f32(((const T *)a.b2x)[(int64_t)seg * d + (n0 + e < d ? n0 + e : d - 1)]);
         }
         for (int t0 = 0; t0 < n_all; t0 += 16) {             // up to sixteen tokens at a time, four to a product
-            constexpr int TT = 4, AHEAD = 8;
+            constexpr int TT = 4, AHEAD = sizeof(T) == 2 ? 8 : 4;
             int at[TT];
 #pragma unroll
             for (int u = 0; u < TT; ++u) at[u] = t0 + u * 4 + q4 < n_all ? slots[wave][t0 + u * 4 + q4] : -1;
@@ -527,7 +527,8 @@ FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
     w.segs = w.by_slot ? pairs : D.P * m.n_experts;
     // a workgroup per compute unit: each routes for itself, so more of them would do that more often
     w.slices = std::max(1, 256 / w.segs);
-    w.groups = w.Fp / 16 >= 4 * w.slices ? 4 : 1;
+    const int together = D.dtype == SF_BF16 ? 4 : 2;          // fp32 weights take twice the registers
+    w.groups = w.Fp / 16 >= together * w.slices ? together : 1;
     w.slices = std::min(ceil_div(w.Fp / 16, w.groups), w.slices);
     w.parts = std::max(1, DOWN_WAVES / w.segs);
     w.route = c.take<uint64_t>((size_t)T);
@@ -592,9 +593,9 @@ extern "C" int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_comp
     a.tile_rows = a.T * row <= XT_BYTES ? a.T : std::min(a.T, TILE_T);
     const size_t lds = a.tile_rows * row + ((size_t)WAVES * 64 * (TILE_T + 1) + (size_t)a.T * (a.E + 1)) * sizeof(float);
     const bool bf = D.dtype == SF_BF16;
-    auto kern = w.groups == 4 ? (bf ? moe_few_up_kernel<h16, 4> : moe_few_up_kernel<float, 4>) : (bf ? moe_few_up_kernel<h16, 1> : moe_few_up_kernel<float, 1>);
+    auto kern = w.groups > 1 ? (bf ? moe_few_up_kernel<h16, 4> : moe_few_up_kernel<float, 2>) : (bf ? moe_few_up_kernel<h16, 1> : moe_few_up_kernel<float, 1>);
     static std::atomic<bool> attr_set[4];         // setting the attribute twice is harmless
-    const int which = bf + 2 * (w.groups == 4);
+    const int which = bf + 2 * (w.groups > 1);
     if (!attr_set[which]) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024) != hipSuccess)
             return fail(SF_ERR_HIP, "moe_ffn_few: cannot reserve LDS");
