@@ -106,6 +106,7 @@ struct GemmI8 {
     float *part;                                                         // I8_AMAX out, I8_CODES in: [n_parts, B L] largest |value| of a
                                                                          // row over each tile of features
     int8_t *codes; float *scale;                                         // I8_CODES: [B L, N] and the row's scale
+    float *top;                                                          // I8_CODES: scratch, [B L]
 };
 int gemm_i8_parts(const GemmI8 &a);                                      // n_parts
 int32_t gemm_i8(I8Mode mode, const GemmI8 &a, hipStream_t st);

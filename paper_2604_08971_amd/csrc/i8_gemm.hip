@@ -16,6 +16,83 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) int i32x16;
 typedef __attribute__((address_space(3))) void lds_void;
 
+// A value that is the same in all lanes, where the compiler does not see it
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+
+// Between stages: this wave's LDS reads have returned.  Not __syncthreads() nor a fence of LDS alone: both wait for the fetches into LDS of later stages.
+__device__ __forceinline__ void barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The largest |activation| of a lane's values, as bits (a NaN is larger than everything).  GELU is evaluated at three of them: |gelu| rises up to its
+// bump at z = -0.7518, falls to 0 and rises again, so its largest value is at the largest z or next to the bump, from either side.
+template <int ACT> struct Largest {
+    uint32_t m = 0;
+    __device__ __forceinline__ void take(float z) { const uint32_t u = ACT == ACT_RELU ? __float_as_uint(z < 0.f ? 0.f : z) & 0x7fffffffu : abs_bits(z); m = m > u ? m : u; }
+    __device__ __forceinline__ uint32_t bits() const { return m; }
+};
+template <> struct Largest<ACT_GELU> {
+    float top = -INFINITY, below = -INFINITY, above = INFINITY, bad = 0.f;
+    __device__ __forceinline__ void take(float z)
+    {
+        top = fmaxf(top, z);
+        below = fmaxf(below, z <= -0.7518f ? z : -INFINITY);
+        above = fminf(above, z >= -0.7518f ? z : INFINITY);
+        bad = fmaf(z, 0.f, bad);                             // NaN from a NaN or an infinity: both make codes of NaN
+    }
+    __device__ __forceinline__ uint32_t bits() const
+    {
+        if (!(bad == 0.f)) return 0x7fc00000u;
+        float m = top > 0.f ? gelu_erf(top) : 0.f;
+        if (below > -INFINITY) m = fmaxf(m, fabsf(gelu_erf(below)));
+        if (above < INFINITY) m = fmaxf(m, fabsf(gelu_erf(above)));
+        return __float_as_uint(m);
+    }
+};
+
+// Four features from n on of a row of fp32
+__device__ __forceinline__ void store4(float *row, int n, int N, f32x4 z)
+{
+    float *C = row + n;
+    if (n + 4 <= N && !((uintptr_t)C & 15)) *reinterpret_cast<f32x4 *>(C) = z;
+    else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (n + e < N) C[e] = z[e];
+    }
+}
+// A lane has four features of every eight of a block of 32, its other half the others: swapped, each has sixteen bytes in a row.
+// Codes, four to a word (N % 64 == 0)
+__device__ __forceinline__ void store_codes(const GemmI8 &a, const uint32_t *w, int64_t row, int n32, int hi, bool there)
+{
+    const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const int n = n32 + hi * 16;
+    if (there && n < a.N) *reinterpret_cast<uint4 *>(a.codes + row * a.N + n) = make_uint4(x[0], x[1], y[0], y[1]);
+}
+// 16-bit values, two to a word
+__device__ __forceinline__ void store_halves(const GemmI8 &a, const uint32_t *w, int64_t row, int n32, int hi, bool there)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const auto x = __builtin_amdgcn_permlane32_swap(w[4 * h], w[4 * h + 2], false, false), y = __builtin_amdgcn_permlane32_swap(w[4 * h + 1], w[4 * h + 3], false, false);
+        const int n = n32 + h * 16 + hi * 8;
+        h16 *C = (h16 *)a.C + row * a.ldc + n;
+        const uint4 o = make_uint4(x[0], y[0], x[1], y[1]);
+        if (!there) continue;
+        if (n + 8 <= a.N && !((uintptr_t)C & 15)) *reinterpret_cast<uint4 *>(C) = o;
+        else {
+            const h16x8 v = __builtin_bit_cast(h16x8, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (n + e < a.N) C[e] = v[e];
+        }
+    }
+}
+
 // BM x BN values a workgroup, WM x WN waves, NS stages of 128 bytes of K in LDS
 template <int BM, int BN, int WM, int WN, int NS, int MODE, int ACT, class TC>
 __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tiles_n, int tiles_l, int n_parts)
@@ -87,7 +164,7 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
     int slot = 0, ahead = NS - 1;
     for (int kt = 0; kt < kts; ++kt) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * (LX + LW)) : "memory");
-        lds_barrier();                                       // stage kt is there, and nobody reads the one before it any more
+        barrier();                                       // stage kt is there, and nobody reads the one before it any more
         fetch(kt + NS - 1, ahead);
         const char *xs = lds + slot * STAGE + (wm * TM * 32 + r) * BK, *ws = lds + slot * STAGE + (BM + wn * TN * 32 + r) * BK;
 #pragma unroll
@@ -114,7 +191,7 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
         const bool there = li < rows;
         const int64_t row = row0 + li;
         [[maybe_unused]] float cr = 0.f;
-        [[maybe_unused]] uint32_t most = 0;
+        [[maybe_unused]] Largest<ACT> most;
         if constexpr (MODE == I8_CODES) {
             // below 2^-100 a row counts as zeros: 127 / amax would overflow
             const uint32_t m = there ? red[li] : 0;
@@ -129,10 +206,14 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
                 const f32x4 s = *reinterpret_cast<const f32x4 *>(sws + nl), bv = *reinterpret_cast<const f32x4 *>(bs + nl);
                 f32x4 z;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[e] = activate<TC>(ACT, (float)acc[i][j][q * 4 + e] * sa[i] * s[e] + bv[e]);
+                for (int e = 0; e < 4; ++e) z[e] = fmaf((float)acc[i][j][q * 4 + e] * sa[i], s[e], bv[e]);
+                if constexpr (MODE != I8_AMAX) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] = activate<TC>(ACT, z[e]);
+                }
                 if constexpr (MODE == I8_AMAX) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { const uint32_t u = abs_bits(z[e]); most = most > u ? most : u; }
+                    for (int e = 0; e < 4; ++e) most.take(z[e]);
                 } else if constexpr (MODE == I8_CODES) {
                     // a value at the border of two codes carries the rounding of its own fp32 sum: no exact decision here
                     int c[4];
@@ -146,40 +227,15 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
                         for (int e = 0; e < 4; ++e) z[e] += rv[e];
                     }
                     if constexpr (sizeof(TC) == 2) { w[2 * q] = pack2_h16(z[0], z[1]); w[2 * q + 1] = pack2_h16(z[2], z[3]); }
-                    else if (there) {
-                        float *C = (float *)a.C + row * a.ldc + n;
-                        if (n + 4 <= a.N && !((uintptr_t)C & 15)) *reinterpret_cast<f32x4 *>(C) = z;
-                        else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) if (n + e < a.N) C[e] = z[e];
-                        }
-                    }
+                    else if (there) store4((float *)a.C + row * a.ldc, n, a.N, z);
                 }
             }
-            // a lane has four features of every eight, its other half the others: swapped, each has sixteen bytes in a row
-            if constexpr (MODE == I8_CODES) {
-                const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-                const int n = n0 + (wn * TN + j) * 32 + hi * 16;
-                if (there && n < a.N) *reinterpret_cast<uint4 *>(a.codes + row * a.N + n) = make_uint4(x[0], x[1], y[0], y[1]);      // N % 64 == 0
-            } else if constexpr (MODE == I8_OUT && sizeof(TC) == 2) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const auto x = __builtin_amdgcn_permlane32_swap(w[4 * h], w[4 * h + 2], false, false), y = __builtin_amdgcn_permlane32_swap(w[4 * h + 1], w[4 * h + 3], false, false);
-                    const int n = n0 + (wn * TN + j) * 32 + h * 16 + hi * 8;
-                    h16 *C = (h16 *)a.C + row * a.ldc + n;
-                    const uint4 o = make_uint4(x[0], y[0], x[1], y[1]);
-                    if (!there) continue;
-                    if (n + 8 <= a.N && !((uintptr_t)C & 15)) *reinterpret_cast<uint4 *>(C) = o;
-                    else {
-                        const h16x8 v = __builtin_bit_cast(h16x8, o);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) if (n + e < a.N) C[e] = v[e];
-                    }
-                }
-            }
+            if constexpr (MODE == I8_CODES) store_codes(a, w, row, n0 + (wn * TN + j) * 32, hi, there);
+            else if constexpr (MODE == I8_OUT && sizeof(TC) == 2) store_halves(a, w, row, n0 + (wn * TN + j) * 32, hi, there);
         }
         if constexpr (MODE == I8_AMAX) {
-            const auto o = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+            const uint32_t m = most.bits();
+            const auto o = __builtin_amdgcn_permlane32_swap(m, m, false, false);
             if (hi == 0) red[wn * BM + li] = o[0] > o[1] ? o[0] : o[1];
         }
     }
@@ -193,6 +249,201 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
         }
     }
 #endif
+}
+
+// Many rows, short K, codes out: the weights stay in registers.  One wave per SIMD holds TF x 32 features whole (KS steps of 32 bytes of K: 24 of
+// three blocks are 288 of its 512 registers), and every 32 rows pass by it once, through LDS.  A tile kernel reads a row and a feature fragment
+// from LDS for every two or four products; here a row fragment serves TF of them and the features none.  The values of one step are finished (scales,
+// activation, codes) between the products of the next, into whose accumulators they do not go.  A workgroup owns a group of features and a run of
+// rows; where the run comes to a sample of another pattern the weights are fetched again.
+// Waiting: a wave's memory operations complete in order as far as vmcnt tells, and it issues the same number each step: F fetches into LDS, then E
+// stores (out of range where there is nothing to store).
+template <int KS, int TF, int MODE, int ACT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_steps)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    static_assert(MODE != I8_OUT, "codes, or their rows' largest values");
+    constexpr int RB = KS * 32, TILE = 32 * RB, SLOT = TILE + 512, NS = KS <= 16 ? 6 : 4, CH = KS * 2, NF = 4 * TF * 32;
+    constexpr int F = KS / 4 + (MODE == I8_CODES ? 2 : 1), E = MODE == I8_CODES ? TF : 1;
+    extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][32 rows of codes, 64 scales, 64 largest values]
+    __shared__ __attribute__((aligned(16))) float sws[NF], bs[NF];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, hi = lane >> 5;
+    const int group = blockIdx.x % groups, at = blockIdx.x / groups, blocks = gridDim.x / groups;
+    const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)total_steps * at / blocks));
+    const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)total_steps * (at + 1) / blocks));
+    if (first >= last) return;
+    const int64_t all_rows = a.B * a.L;
+    const int f0 = group * per * TF * 32, n0 = f0 + wave * TF * 32;
+    const bool works = wave < per && n0 < a.N;
+    struct Step { int64_t row0; int b, rows; };
+    auto step_of = [&](int s) {
+        const int b = s / steps_l, i0 = (s - b * steps_l) * 32;
+        const int64_t left = a.L - i0;
+        return Step{uniform(b * a.L + i0), b, __builtin_amdgcn_readfirstlane(left < 32 ? (int)left : 32)};
+    };
+    // a wave fetches KS / 4 KB of the 32 rows; chunk c of row r lies at c ^ (r % 8), so that 16 lanes of a fragment read meet no bank twice
+    int off[KS / 4];
+#pragma unroll
+    for (int j = 0; j < KS / 4; ++j) {
+        const int q = (j * 4 + wave) * 64 + lane, row = q / CH, chunk = (q - row * CH) ^ (row & 7);
+        off[j] = chunk * 16 < a.K ? row * (int)a.lda + chunk * 16 : 0x7ffffff0;
+    }
+    auto fetch = [&](int s, int slot) {
+        const Step st = step_of(s < last ? s : last - 1);
+        const int rows = s < last ? st.rows : 0;             // past the end: zeros
+        char *base = lds + slot * SLOT;
+        const auto ar = __builtin_amdgcn_make_buffer_rsrc((void *)(a.A + uniform(st.row0 * a.lda)), 0, __builtin_amdgcn_readfirstlane(rows ? (rows - 1) * (int)a.lda + a.K : 0), 0x00020000);
+        const auto sr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.sa + uniform(st.row0)), 0, rows * 4, 0x00020000);
+#pragma unroll
+        for (int j = 0; j < KS / 4; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(base + (j * 4 + wave) * 1024), 16, off[j], 0, 0, 0);
+        // every wave brings the same 32 values (and 32 zeros): the count of its operations is what matters
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, (lds_void *)(base + TILE), 4, lane * 4, 0, 0, 0);
+        if constexpr (MODE == I8_CODES) {
+            const auto tr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.top + uniform(st.row0)), 0, rows * 4, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, (lds_void *)(base + TILE + 256), 4, lane * 4, 0, 0, 0);
+        }
+    };
+    i32x4 w[TF][KS];
+    auto weights = [&](int p) {
+        const int8_t *W = a.W + p * a.w_pstride;
+#pragma unroll
+        for (int j = 0; j < TF; ++j) {
+            const int n = n0 + j * 32 + r;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                w[j][k] = i32x4{0, 0, 0, 0};
+                if (works && n < a.N && (k * 2 + hi) * 16 < a.K) w[j][k] = *reinterpret_cast<const i32x4 *>(W + n * a.ldw + (k * 2 + hi) * 16);
+            }
+        }
+        for (int i = threadIdx.x; i < NF; i += 256) {
+            const int n = f0 + i;
+            sws[i] = n < a.N ? a.sw[p * a.sw_pstride + n] : 0.f;
+            bs[i] = n >= a.N || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n];
+        }
+    };
+    i32x16 done[TF];                                         // the last step's sums, its rows and what belongs to them
+    Step prev{0, 0, 0};
+    float sa = 0.f, cr = 0.f;
+    [[maybe_unused]] Largest<ACT> most;
+    [[maybe_unused]] uint32_t o[4];
+    f32x4 sv, bv;
+    auto scales = [&](int j, int q) {
+        const int nl = (wave * TF + j) * 32 + q * 8 + hi * 4;
+        sv = *reinterpret_cast<const f32x4 *>(sws + nl);
+        bv = *reinterpret_cast<const f32x4 *>(bs + nl);
+    };
+    auto quad = [&](int j, int q) {                          // four features of the last step's rows
+        f32x4 z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = fmaf((float)done[j][q * 4 + e] * sa, sv[e], bv[e]);
+        if constexpr (MODE == I8_AMAX) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most.take(z[e]);
+        } else {
+            int c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = (int)__builtin_rintf(activate<h16>(ACT, z[e]) * cr);
+            o[q] = pack4_i8(c[0], c[1], c[2], c[3]);
+            if (q == 3) {
+                const auto x = __builtin_amdgcn_permlane32_swap(o[0], o[2], false, false), y = __builtin_amdgcn_permlane32_swap(o[1], o[3], false, false);
+                const int n = n0 + j * 32 + hi * 16;
+                const auto cr_ = __builtin_amdgcn_make_buffer_rsrc((void *)(a.codes + uniform(prev.row0 * a.N)), 0, prev.rows * a.N, 0x00020000);
+                const bool in = works && r < prev.rows && n < a.N;
+                __builtin_amdgcn_raw_buffer_store_b128(i32x4{(int)x[0], (int)x[1], (int)y[0], (int)y[1]}, cr_, in ? r * a.N + n : 0x7ffffff0, 0, 0);
+            }
+        }
+    };
+    auto finish = [&]() {                                    // the last step's rows: their largest values
+        if constexpr (MODE == I8_AMAX) {
+            const uint32_t m = most.bits();
+            const auto x = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+            const auto pr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.part + uniform((group * per + wave) * all_rows + prev.row0)), 0, prev.rows * 4, 0x00020000);
+            __builtin_amdgcn_raw_buffer_store_b32((int)(x[0] > x[1] ? x[0] : x[1]), pr, works && hi == 0 ? r * 4 : 0x7ffffff0, 0, 0);
+            most = Largest<ACT>();
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < TF; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) done[j][e] = 0;
+    for (int s = 0; s < NS - 1; ++s) fetch(first + s, s);
+    int slot = 0, ahead = NS - 1, p_at = -1;
+    for (int s = first; s < last; ++s) {
+        const Step st = step_of(s);
+        const int p = a.P > 1 && a.pattern_id ? a.pattern_id[st.b] : 0;
+        if (p != p_at) {
+            if (p_at >= 0) {                                 // the last pattern's scales are still wanted
+#pragma unroll
+                for (int j = 0; j < TF; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) { scales(j, q); quad(j, q); }
+                finish();
+                prev.rows = 0;
+                barrier();
+            }
+            weights(p);
+            p_at = p;
+            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0), as the compiler understands it: it would wait for the weights at their use
+        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(E + (NS - 2) * (F + E) < 63 ? E + (NS - 2) * (F + E) : 63) : "memory");
+        barrier();                                       // step s is there, and nobody reads the one before it any more
+        fetch(s + NS - 1, ahead);
+        const char *xs = lds + slot * SLOT + r * RB;
+        const float *xsc = reinterpret_cast<const float *>(lds + slot * SLOT + TILE);
+        const float sa_now = xsc[r];
+        [[maybe_unused]] const float top_now = MODE == I8_CODES ? xsc[64 + r] : 0.f;
+        i32x16 acc[TF];
+#pragma unroll
+        for (int j = 0; j < TF; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[j][e] = 0;
+        i32x4 xf[2];
+        xf[0] = *reinterpret_cast<const i32x4 *>(xs + (hi ^ (r & 7)) * 16);
+        scales(0, 0);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            if (k + 1 < KS) xf[(k + 1) & 1] = *reinterpret_cast<const i32x4 *>(xs + (((k + 1) * 2 + hi) ^ (r & 7)) * 16);
+#pragma unroll
+            for (int j = 0; j < TF; ++j) acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j][k], xf[k & 1], acc[j], 0, 0, 0);
+            // 4 TF quads over the KS steps
+#pragma unroll
+            for (int q = 4 * TF * k / KS; q < 4 * TF * (k + 1) / KS; ++q) {
+                quad(q / 4, q % 4);
+                if (q + 1 < 4 * TF) scales((q + 1) / 4, (q + 1) % 4);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        finish();
+#pragma unroll
+        for (int j = 0; j < TF; ++j) done[j] = acc[j];
+        prev = st;
+        sa = sa_now;
+        if constexpr (MODE == I8_CODES)                      // below 2^-100 a row counts as zeros: 127 / amax would overflow
+            cr = __float_as_uint(top_now) < 0x7f800000u && top_now >= 0x1p-100f ? 127.0f / top_now : 0.f;
+        slot = slot + 1 == NS ? 0 : slot + 1;
+        ahead = ahead + 1 == NS ? 0 : ahead + 1;
+    }
+#pragma unroll
+    for (int j = 0; j < TF; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) { scales(j, q); quad(j, q); }
+    finish();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the zeros past the end are in LDS: the launch's memory is its own again
+#endif
+}
+
+// The largest of a row's parts, and the row's scale
+__global__ __launch_bounds__(256) void i8_top_kernel(const float *__restrict__ part, int n_parts, int64_t rows, float *__restrict__ top, float *__restrict__ scale)
+{
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row >= rows) return;
+    uint32_t m = 0;
+#pragma unroll 8
+    for (int q = 0; q < n_parts; ++q) { const uint32_t u = __float_as_uint(part[q * rows + row]); m = m > u ? m : u; }
+    top[row] = __uint_as_float(m);
+    scale[row] = m < 0x7f800000u ? __uint_as_float(m) / 127.0f : __uint_as_float(0x7fc00000u);
 }
 
 template <int BM, int BN, int WM, int WN, int NS, int MODE, int ACT, class TC>
@@ -228,9 +479,58 @@ Tile tile_of(const GemmI8 &a)
     auto tiles = [&](int m, int n) { return samples * ((L + m - 1) / m) * ((a.N + n - 1) / n); };
     return tiles(128, 128) >= 256 ? BIG : tiles(64, 64) >= 256 ? MIDDLE : SMALL;
 }
+
+// The kernel with held weights, by K: three or four blocks of features a wave up to 768, two up to 1024; rows enough for some steps of 32 per workgroup
+struct Held { int ks, tf, groups, per, steps_l; int64_t steps; };
+bool held(const GemmI8 &a, Held &h)
+{
+    const int64_t samples = a.P > 1 ? a.B : 1, L = a.P > 1 ? a.L : a.B * a.L;
+    if (a.K > 1024 || a.lda > 1 << 20 || (L + 31) / 32 > 1 << 24) return false;
+    h.ks = a.K <= 256 ? 8 : a.K <= 512 ? 16 : a.K <= 768 ? 24 : 32;
+    h.tf = h.ks <= 16 ? 4 : h.ks == 24 ? 3 : 2;
+    const int units = ceil_div(a.N, h.tf * 32);
+    h.groups = ceil_div(units, 4);
+    h.per = ceil_div(units, h.groups);
+    h.steps_l = (int)((L + 31) / 32);
+    h.steps = samples * h.steps_l;
+    return h.steps <= 1 << 30 && h.groups <= 64 && h.steps * h.groups >= 256 * 4;
+}
+template <int KS, int TF, int MODE, int ACT>
+int32_t launch_held(const GemmI8 &a, const Held &h, hipStream_t st)
+{
+    auto kern = gemm_i8_held_kernel<KS, TF, MODE, ACT>;
+    constexpr int LDS = (KS <= 16 ? 6 : 4) * (KS * 1024 + 512);
+    static std::atomic<bool> attr_set{false};     // setting the attribute twice is harmless
+    if (!attr_set) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
+            return fail(SF_ERR_HIP, "gemm_i8: cannot reserve LDS");
+        attr_set = true;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)(256 / h.groups * h.groups)), dim3(256), LDS, st, a, h.groups, h.per, h.steps_l, (int)h.steps);
+    return check_launch("gemm_i8");
+}
+template <int MODE, int ACT>
+int32_t launch_held_k(const GemmI8 &a, const Held &h, hipStream_t st)
+{
+    switch (h.ks) {
+    case 8: return launch_held<8, 4, MODE, ACT>(a, h, st);
+    case 16: return launch_held<16, 4, MODE, ACT>(a, h, st);
+    case 24: return launch_held<24, 3, MODE, ACT>(a, h, st);
+    default: return launch_held<32, 2, MODE, ACT>(a, h, st);
+    }
+}
+
 template <int MODE, class TC>
 int32_t launch_tile(const GemmI8 &a, hipStream_t st)
 {
+    if constexpr (MODE != I8_OUT) {
+        Held h;
+        if (held(a, h)) {
+            if (MODE == I8_CODES)
+                hipLaunchKernelGGL(i8_top_kernel, dim3((unsigned)((a.B * a.L + 255) / 256)), dim3(256), 0, st, a.part, gemm_i8_parts(a), a.B * a.L, a.top, a.scale);
+            return a.act == ACT_GELU ? launch_held_k<MODE, ACT_GELU>(a, h, st) : launch_held_k<MODE, ACT_RELU>(a, h, st);
+        }
+    }
     switch (tile_of(a)) {
     case BIG: return launch_act<128, 128, 2, 2, 2, MODE, TC>(a, st);
     case MIDDLE: return launch_act<64, 64, 2, 2, 4, MODE, TC>(a, st);
@@ -240,7 +540,11 @@ int32_t launch_tile(const GemmI8 &a, hipStream_t st)
 
 }  // namespace
 
-int gemm_i8_parts(const GemmI8 &a) { return ceil_div(a.N, tile_of(a) == BIG ? 128 : 64); }
+int gemm_i8_parts(const GemmI8 &a)
+{
+    Held h;
+    return held(a, h) ? ceil_div(a.N, h.tf * 32) : ceil_div(a.N, tile_of(a) == BIG ? 128 : 64);
+}
 
 int32_t gemm_i8(I8Mode mode, const GemmI8 &a0, hipStream_t st)
 {

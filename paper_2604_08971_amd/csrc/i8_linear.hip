@@ -188,7 +188,7 @@ LinearWs linear_ws(int64_t rows, int K, void *ws)
 }
 
 // Few rows: hid holds them in fp32 between the two launches
-struct FfnI8Ws { int8_t *xq, *hq; float *sx, *sh, *part, *hid; size_t bytes; };
+struct FfnI8Ws { int8_t *xq, *hq; float *sx, *sh, *part, *top, *hid; size_t bytes; };
 bool ffn_few(const Dims &D, int Fp) { return D.d <= FEW_K && Fp <= FEW_K && (D.P > 1 ? D.L <= FEW_ROWS && D.B <= 8 : (int64_t)D.B * D.L <= FEW_ROWS); }
 FfnI8Ws ffn_ws(const Dims &D, int Fp, void *ws)
 {
@@ -199,7 +199,8 @@ FfnI8Ws ffn_ws(const Dims &D, int Fp, void *ws)
     w.sx = c.take<float>(rows);
     w.hq = c.take<int8_t>(rows * Fp);
     w.sh = c.take<float>(rows);
-    w.part = c.take<float>(rows * ceil_div(Fp, 64));
+    w.part = c.take<float>(rows * ceil_div(Fp, 32));      // the most parts that any kernel makes
+    w.top = c.take<float>(rows);
     w.hid = ffn_few(D, Fp) ? c.take<float>(rows * Fp) : nullptr;
     w.bytes = c.off;
     return w;
@@ -317,7 +318,7 @@ extern "C" int32_t sf_pruned_ffn_i8_forward(const sf_desc *desc, const sf_ffn_i8
     GemmI8 u{};
     u.A = w.xq; u.lda = D.d; u.sa = w.sx; u.W = f->W1q; u.ldw = D.d; u.w_pstride = (int64_t)Fp * D.d; u.sw = f->s1; u.sw_pstride = Fp;
     u.bias = f->b1; u.bias_pstride = Fp; u.pattern_id = pattern_id; u.P = D.P; u.B = D.B; u.L = D.L; u.N = Fp; u.K = D.d; u.act = act_of(D.act);
-    u.part = w.part; u.codes = w.hq; u.scale = w.sh;
+    u.part = w.part; u.top = w.top; u.codes = w.hq; u.scale = w.sh;
     if (int32_t rc = gemm_i8(I8_AMAX, u, st)) return rc;
     if (int32_t rc = gemm_i8(I8_CODES, u, st)) return rc;
     GemmI8 v{};
