@@ -251,6 +251,151 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
 #endif
 }
 
+// Many rows and features, long K: 256 x 256 values a workgroup, 128 x 128 a wave, one wave per SIMD.  A wave then reads eight fragments for sixteen products
+// and the LDS keeps ahead of the matrix cores (1536 of 2048 clocks per 128 bytes of K, with its writes; tiles of 128 x 128 need 1536 of 1024).  Stages of
+// 64 bytes of K, four of them; fragments are read one step of 32 bytes ahead, across the stages: the wait for the next one stands in the middle.
+template <int ACT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int BM = 256, BN = 256, BK = 64, NS = 4, LX = 4, LW = 4, STAGE = (BM + BN) * BK;
+    extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][rows, features][64]
+    __shared__ __attribute__((aligned(16))) float sws[BN], bs[BN];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, hi = lane >> 5;
+    const int wm = wave >> 1, wn = wave & 1;
+    // an XCD walks a contiguous run of tiles, the features of a row tile one after the other: its L2 reads the rows once
+    const int total = gridDim.x, q8 = total / 8, r8 = total % 8, xcd = blockIdx.x % 8;
+    const int t = xcd * q8 + (xcd < r8 ? xcd : r8) + blockIdx.x / 8;
+    const int tn = t % tiles_n, tm = t / tiles_n;
+    const int64_t b = tm / tiles_l, i0 = (int64_t)(tm % tiles_l) * BM, row0 = b * a.L + i0, left = a.L - i0;
+    const int rows = left < BM ? (int)left : BM, n0 = tn * BN, feats = a.N - n0 < BN ? a.N - n0 : BN;
+    const int p = a.P > 1 && a.pattern_id ? a.pattern_id[b] : 0;
+    const auto ar = __builtin_amdgcn_make_buffer_rsrc((void *)(a.A + uniform(row0 * a.lda)), 0, __builtin_amdgcn_readfirstlane((rows - 1) * (int)a.lda + a.K), 0x00020000);
+    const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.W + uniform(p * a.w_pstride + (int64_t)n0 * a.ldw)), 0,
+                                                      __builtin_amdgcn_readfirstlane((feats - 1) * (int)a.ldw + a.K), 0x00020000);
+    // piece q of a stage: row q / 4, chunk (q % 4) ^ (row / 2 % 4) of its four, so that 16 lanes of a fragment read meet no bank twice
+    const int chunk = (threadIdx.x & 3) ^ ((threadIdx.x >> 3) & 3);
+    const int xoff = (threadIdx.x >> 2) * (int)a.lda + chunk * 16, woff = (threadIdx.x >> 2) * (int)a.ldw + chunk * 16;
+    const int xstep = 64 * (int)a.lda, wstep = 64 * (int)a.ldw;
+    auto fetch = [&](int kt, int s) {                        // past the last one: zeros
+        char *base = lds + s * STAGE + wave * 1024;
+        const bool in = kt * BK + chunk * 16 < a.K;
+        const int xo = in ? xoff + kt * BK : 0x7ffffff0 - LX * xstep, wo = in ? woff + kt * BK : 0x7ffffff0 - LW * wstep;
+#pragma unroll
+        for (int j = 0; j < LX; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(base + j * 4096), 16, xo + j * xstep, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < LW; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK + j * 4096), 16, wo + j * wstep, 0, 0, 0);
+    };
+    const int kts = (a.K + BK - 1) / BK;
+    const float *sw = a.sw + p * a.sw_pstride;
+    {
+        const int n = threadIdx.x;
+        const bool in = n0 + n < a.N;
+        sws[n] = in ? sw[n0 + n] : 0.f;
+        bs[n] = !in || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n0 + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n0 + n];
+    }
+    float sa[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const int l = (wm * 4 + i) * 32 + r; sa[i] = l < rows ? a.sa[row0 + l] : 0.f; }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): nothing but the stages is counted from here on
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) fetch(s, s);
+    i32x16 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+    const int at[2] = {(hi ^ ((r >> 1) & 3)) * 16, ((2 + hi) ^ ((r >> 1) & 3)) * 16};
+    const int xrow = (wm * 128 + r) * BK, wrow = BM * BK + (wn * 128 + r) * BK;
+    i32x4 xf[2][4], wf[2][4];
+    auto read = [&](int slot, int k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            xf[k][i] = *reinterpret_cast<const i32x4 *>(lds + slot * STAGE + xrow + i * 32 * BK + at[k]);
+            wf[k][i] = *reinterpret_cast<const i32x4 *>(lds + slot * STAGE + wrow + i * 32 * BK + at[k]);
+        }
+    };
+    auto multiply = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[k][j], xf[k][i], acc[i][j], 0, 0, 0);
+    };
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * (LX + LW)) : "memory");
+    barrier();
+    read(0, 0);
+    int slot = 0, ahead = NS - 1;
+    for (int kt = 0; kt < kts; ++kt) {
+        read(slot, 1);
+        __builtin_amdgcn_sched_barrier(0);                   // in this order: the reads return while the products run
+        multiply(0);
+        __builtin_amdgcn_sched_barrier(0);
+        slot = slot + 1 == NS ? 0 : slot + 1;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 3) * (LX + LW)) : "memory");
+        barrier();                                           // stage kt + 1 is there, and nobody reads kt - 1 any more
+        fetch(kt + NS - 1, ahead);
+        ahead = ahead + 1 == NS ? 0 : ahead + 1;
+        read(slot, 0);                                       // behind the last stage: zeros, multiplied by nobody
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // the zeros past the end are in LDS: the launch's memory is its own again
+    // residual: sixteen bytes in a row of the values' own order, exchanged between the halves as the values are; the next block's on their way
+    const bool whole = a.R && !(a.ldr & 7) && !((uintptr_t)a.R & 15) && n0 + BN <= a.N;
+    uint4 next[2];
+    auto residual = [&](int i, int j) {
+        const int li = (wm * 4 + i) * 32 + r;
+        const h16 *R = (const h16 *)a.R + (row0 + (li < rows ? li : 0)) * a.ldr + n0 + (wn * 4 + j) * 32 + hi * 8;
+        next[0] = *reinterpret_cast<const uint4 *>(R);
+        next[1] = *reinterpret_cast<const uint4 *>(R + 16);
+    };
+    if (whole) residual(0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int li = (wm * 4 + i) * 32 + r;                // row inside the tile
+        const bool there = li < rows;
+        const int64_t row = row0 + li;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t w[8];
+            uint32_t rw[8];
+            if (whole) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const auto x = __builtin_amdgcn_permlane32_swap(next[h].x, next[h].z, false, false), y = __builtin_amdgcn_permlane32_swap(next[h].y, next[h].w, false, false);
+                    rw[4 * h] = x[0]; rw[4 * h + 1] = y[0]; rw[4 * h + 2] = x[1]; rw[4 * h + 3] = y[1];
+                }
+                if (i * 4 + j < 15) residual(j < 3 ? i : i + 1, j < 3 ? j + 1 : 0);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int nl = (wn * 4 + j) * 32 + q * 8 + hi * 4, n = n0 + nl;
+                const f32x4 s = *reinterpret_cast<const f32x4 *>(sws + nl), bv = *reinterpret_cast<const f32x4 *>(bs + nl);
+                f32x4 z;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = activate<h16>(ACT, fmaf((float)acc[i][j][q * 4 + e] * sa[i], s[e], bv[e]));
+                if (whole) {
+                    const h16x4 rv = __builtin_bit_cast(h16x4, make_uint2(rw[2 * q], rw[2 * q + 1]));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] += (float)rv[e];
+                } else if (a.R && there) {
+                    const f32x4 rv = four((const h16 *)a.R + row * a.ldr, n, a.N);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] += rv[e];
+                }
+                w[2 * q] = pack2_h16(z[0], z[1]);
+                w[2 * q + 1] = pack2_h16(z[2], z[3]);
+            }
+            store_halves(a, w, row, n0 + (wn * 4 + j) * 32, hi, there);
+        }
+    }
+#endif
+}
+
 // Many rows, short K, codes out: the weights stay in registers.  One wave per SIMD holds TF x 32 features whole (KS steps of 32 bytes of K: 24 of
 // three blocks are 288 of its 512 registers), and every 32 rows pass by it once, through LDS.  A tile kernel reads a row and a feature fragment
 // from LDS for every two or four products; here a row fragment serves TF of them and the features none.  The values of one step are finished (scales,
@@ -471,12 +616,15 @@ int32_t launch_act(const GemmI8 &a, hipStream_t st)
     return fail(SF_ERR_UNSUPPORTED, "gemm_i8: this mode takes an activation");
 }
 
-// Tiles: 128 x 128 where they give every compute unit one, 64 x 64 or 32 x 64 with more stages ahead where they do not
-enum Tile { BIG, MIDDLE, SMALL };
-Tile tile_of(const GemmI8 &a)
+// Tiles: 256 x 256 where whole rounds of one per compute unit hold at least two thirds of values (and for 16-bit values alone), 128 x 128 where they give every
+// compute unit one, 64 x 64 or 32 x 64 with more stages ahead where they do not
+enum Tile { WIDE, BIG, MIDDLE, SMALL };
+Tile tile_of(const GemmI8 &a, bool values)
 {
     const int64_t samples = a.P > 1 ? a.B : 1, L = a.P > 1 ? a.L : a.B * a.L;
     auto tiles = [&](int m, int n) { return samples * ((L + m - 1) / m) * ((a.N + n - 1) / n); };
+    const int64_t rounds = (tiles(256, 256) + 255) / 256;
+    if (values && 3 * samples * L * a.N >= 2 * rounds * 256 * 65536) return WIDE;
     return tiles(128, 128) >= 256 ? BIG : tiles(64, 64) >= 256 ? MIDDLE : SMALL;
 }
 
@@ -520,6 +668,22 @@ int32_t launch_held_k(const GemmI8 &a, const Held &h, hipStream_t st)
     }
 }
 
+template <int ACT>
+int32_t launch_wide(const GemmI8 &a, hipStream_t st)
+{
+    auto kern = gemm_i8_wide_kernel<ACT>;
+    constexpr int LDS = 4 * 512 * 64;
+    static std::atomic<bool> attr_set{false};     // setting the attribute twice is harmless
+    if (!attr_set) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
+            return fail(SF_ERR_HIP, "gemm_i8: cannot reserve LDS");
+        attr_set = true;
+    }
+    const int64_t tiles_l = (a.L + 255) / 256, tiles_n = (a.N + 255) / 256, grid = a.B * tiles_l * tiles_n;
+    if (grid > 0x7fffffff) return fail(SF_ERR_SHAPE, "gemm_i8: too many tiles");
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), LDS, st, a, (int)tiles_n, (int)tiles_l);
+    return check_launch("gemm_i8");
+}
 template <int MODE, class TC>
 int32_t launch_tile(const GemmI8 &a, hipStream_t st)
 {
@@ -531,7 +695,10 @@ int32_t launch_tile(const GemmI8 &a, hipStream_t st)
             return a.act == ACT_GELU ? launch_held_k<MODE, ACT_GELU>(a, h, st) : launch_held_k<MODE, ACT_RELU>(a, h, st);
         }
     }
-    switch (tile_of(a)) {
+    switch (tile_of(a, MODE == I8_OUT && sizeof(TC) == 2)) {
+    case WIDE:
+        if constexpr (MODE == I8_OUT && sizeof(TC) == 2)
+            return a.act == ACT_GELU ? launch_wide<ACT_GELU>(a, st) : a.act == ACT_RELU ? launch_wide<ACT_RELU>(a, st) : launch_wide<ACT_NONE>(a, st);
     case BIG: return launch_act<128, 128, 2, 2, 2, MODE, TC>(a, st);
     case MIDDLE: return launch_act<64, 64, 2, 2, 4, MODE, TC>(a, st);
     default: return launch_act<32, 64, 1, 2, 5, MODE, TC>(a, st);
@@ -543,7 +710,7 @@ int32_t launch_tile(const GemmI8 &a, hipStream_t st)
 int gemm_i8_parts(const GemmI8 &a)
 {
     Held h;
-    return held(a, h) ? ceil_div(a.N, h.tf * 32) : ceil_div(a.N, tile_of(a) == BIG ? 128 : 64);
+    return held(a, h) ? ceil_div(a.N, h.tf * 32) : ceil_div(a.N, tile_of(a, false) == BIG ? 128 : 64);
 }
 
 int32_t gemm_i8(I8Mode mode, const GemmI8 &a0, hipStream_t st)
