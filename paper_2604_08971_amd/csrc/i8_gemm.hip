@@ -16,6 +16,8 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) int i32x16;
 typedef __attribute__((address_space(3))) void lds_void;
 
+__device__ __forceinline__ float plain_nan(float x) { return x == x ? x : __uint_as_float(0x7fc00000u); }
+
 // A value that is the same in all lanes, where the compiler does not see it
 __device__ __forceinline__ int64_t uniform(int64_t x)
 {
@@ -32,10 +34,11 @@ __device__ __forceinline__ void barrier()
 
 // The largest |activation| of a lane's values, as bits (a NaN is larger than everything).  GELU is evaluated at three of them: |gelu| rises up to its
 // bump at z = -0.7518, falls to 0 and rises again, so its largest value is at the largest z or next to the bump, from either side.
+// ReLU: as integers, negative values are below zero (a NaN comes without a sign: scales and biases are brought to that).
 template <int ACT> struct Largest {
-    uint32_t m = 0;
-    __device__ __forceinline__ void take(float z) { const uint32_t u = ACT == ACT_RELU ? __float_as_uint(z < 0.f ? 0.f : z) & 0x7fffffffu : abs_bits(z); m = m > u ? m : u; }
-    __device__ __forceinline__ uint32_t bits() const { return m; }
+    int m = 0;
+    __device__ __forceinline__ void take(float z) { const int u = __float_as_int(z); m = m > u ? m : u; }
+    __device__ __forceinline__ uint32_t bits() const { return (uint32_t)m; }
 };
 template <> struct Largest<ACT_GELU> {
     float top = -INFINITY, below = -INFINITY, above = INFINITY, bad = 0.f;
@@ -140,8 +143,8 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
     const float *sw = a.sw + p * a.sw_pstride;
     for (int n = threadIdx.x; n < BN; n += NT) {
         const bool in = n0 + n < a.N;
-        sws[n] = in ? sw[n0 + n] : 0.f;
-        bs[n] = !in || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n0 + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n0 + n];
+        sws[n] = in ? plain_nan(sw[n0 + n]) : 0.f;
+        bs[n] = !in || !a.bias ? 0.f : plain_nan(a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n0 + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n0 + n]);
     }
     float sa[TM];
 #pragma unroll
@@ -251,146 +254,171 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
 #endif
 }
 
-// Many rows and features, long K: 256 x 256 values a workgroup, 128 x 128 a wave, one wave per SIMD.  A wave then reads eight fragments for sixteen products
-// and the LDS keeps ahead of the matrix cores (1536 of 2048 clocks per 128 bytes of K, with its writes; tiles of 128 x 128 need 1536 of 1024).  Stages of
-// 64 bytes of K, four of them; fragments are read one step of 32 bytes ahead, across the stages: the wait for the next one stands in the middle.
+// Many rows and features: 128 x 256 values a workgroup, 64 x 128 a wave (six fragment reads for eight products), two workgroups per compute unit, of
+// which one finishes its tile while the other multiplies.  K in steps of 32 bytes, six of them in LDS, four on their way: 96 KB a compute unit, what the
+// latency of memory wants (256 x 256 values with 64 KB on their way took 2100 clocks for 1024 of products).  Fragments are read one step ahead.
 template <int ACT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
-void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l)
+__global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int BM = 256, BN = 256, BK = 64, NS = 4, LX = 4, LW = 4, STAGE = (BM + BN) * BK;
-    extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][rows, features][64]
+    constexpr int BM = 128, BN = 256, BK = 32, NS = 6, STAGE = (BM + BN) * BK;
+    extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][rows, features][32]
     __shared__ __attribute__((aligned(16))) float sws[BN], bs[BN];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, hi = lane >> 5;
-    const int wm = wave >> 1, wn = wave & 1;
+    const int wm = wave >> 1, wn = wave & 1, kts = (a.K + BK - 1) / BK;
     // an XCD walks a contiguous run of tiles, the features of a row tile one after the other: its L2 reads the rows once
     const int total = gridDim.x, q8 = total / 8, r8 = total % 8, xcd = blockIdx.x % 8;
     const int t = xcd * q8 + (xcd < r8 ? xcd : r8) + blockIdx.x / 8;
     const int tn = t % tiles_n, tm = t / tiles_n;
-    const int64_t b = tm / tiles_l, i0 = (int64_t)(tm % tiles_l) * BM, row0 = b * a.L + i0, left = a.L - i0;
-    const int rows = left < BM ? (int)left : BM, n0 = tn * BN, feats = a.N - n0 < BN ? a.N - n0 : BN;
-    const int p = a.P > 1 && a.pattern_id ? a.pattern_id[b] : 0;
+    const int64_t b = tm / tiles_l, i0 = (int64_t)(tm % tiles_l) * BM, row0 = uniform(b * a.L + i0), left = a.L - i0;
+    const int rows = __builtin_amdgcn_readfirstlane(left < BM ? (int)left : BM), n0 = tn * BN, feats = a.N - n0 < BN ? a.N - n0 : BN;
+    const int p = a.P > 1 && a.pattern_id ? __builtin_amdgcn_readfirstlane(a.pattern_id[b]) : 0;
     const auto ar = __builtin_amdgcn_make_buffer_rsrc((void *)(a.A + uniform(row0 * a.lda)), 0, __builtin_amdgcn_readfirstlane((rows - 1) * (int)a.lda + a.K), 0x00020000);
     const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.W + uniform(p * a.w_pstride + (int64_t)n0 * a.ldw)), 0,
                                                       __builtin_amdgcn_readfirstlane((feats - 1) * (int)a.ldw + a.K), 0x00020000);
-    // piece q of a stage: row q / 4, chunk (q % 4) ^ (row / 2 % 4) of its four, so that 16 lanes of a fragment read meet no bank twice
-    const int chunk = (threadIdx.x & 3) ^ ((threadIdx.x >> 3) & 3);
-    const int xoff = (threadIdx.x >> 2) * (int)a.lda + chunk * 16, woff = (threadIdx.x >> 2) * (int)a.ldw + chunk * 16;
-    const int xstep = 64 * (int)a.lda, wstep = 64 * (int)a.ldw;
+    // piece q of a stage: row q / 2, chunk (q % 2) ^ (row / 4 % 2) of its two, so that 16 lanes of a fragment read meet no bank twice
+    const int chunk = (threadIdx.x & 1) ^ ((threadIdx.x >> 3) & 1);
+    const int xoff = (threadIdx.x >> 1) * (int)a.lda + chunk * 16, woff = (threadIdx.x >> 1) * (int)a.ldw + chunk * 16, wstep = 128 * (int)a.ldw;
     auto fetch = [&](int kt, int s) {                        // past the last one: zeros
         char *base = lds + s * STAGE + wave * 1024;
         const bool in = kt * BK + chunk * 16 < a.K;
-        const int xo = in ? xoff + kt * BK : 0x7ffffff0 - LX * xstep, wo = in ? woff + kt * BK : 0x7ffffff0 - LW * wstep;
-#pragma unroll
-        for (int j = 0; j < LX; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(base + j * 4096), 16, xo + j * xstep, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < LW; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK + j * 4096), 16, wo + j * wstep, 0, 0, 0);
+        const int xo = in ? xoff + kt * BK : 0x7ffffff0, wo = in ? woff + kt * BK : 0x7ffffff0 - wstep;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)base, 16, xo, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK), 16, wo, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK + 4096), 16, wo + wstep, 0, 0, 0);
     };
-    const int kts = (a.K + BK - 1) / BK;
-    const float *sw = a.sw + p * a.sw_pstride;
-    {
-        const int n = threadIdx.x;
-        const bool in = n0 + n < a.N;
-        sws[n] = in ? sw[n0 + n] : 0.f;
-        bs[n] = !in || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n0 + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n0 + n];
-    }
-    float sa[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const int l = (wm * 4 + i) * 32 + r; sa[i] = l < rows ? a.sa[row0 + l] : 0.f; }
-    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): nothing but the stages is counted from here on
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) fetch(s, s);
-    i32x16 acc[4][4];
+    {
+        const int n = n0 + threadIdx.x;
+        const bool in = n < a.N;
+        sws[threadIdx.x] = in ? a.sw[p * a.sw_pstride + n] : 0.f;
+        bs[threadIdx.x] = !in || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n];
+    }
+    float sa[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i) { const int l = (wm * 2 + i) * 32 + r; sa[i] = l < rows ? a.sa[row0 + l] : 0.f; }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): from here on the compiler has nothing of its own to wait for
+    i32x16 acc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    const int at[2] = {(hi ^ ((r >> 1) & 3)) * 16, ((2 + hi) ^ ((r >> 1) & 3)) * 16};
-    const int xrow = (wm * 128 + r) * BK, wrow = BM * BK + (wn * 128 + r) * BK;
-    i32x4 xf[2][4], wf[2][4];
-    auto read = [&](int slot, int k) {
+    const int pos = (hi ^ ((r >> 2) & 1)) * 16, xrow = (wm * 64 + r) * BK + pos, wrow = BM * BK + (wn * 128 + r) * BK + pos;
+    i32x4 xf[2][2], wf[2][4];
+    auto read = [&](int slot, int f) {
+        const char *base = lds + slot * STAGE;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            xf[k][i] = *reinterpret_cast<const i32x4 *>(lds + slot * STAGE + xrow + i * 32 * BK + at[k]);
-            wf[k][i] = *reinterpret_cast<const i32x4 *>(lds + slot * STAGE + wrow + i * 32 * BK + at[k]);
-        }
+        for (int i = 0; i < 2; ++i) xf[f][i] = *reinterpret_cast<const i32x4 *>(base + xrow + i * 32 * BK);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) wf[f][j] = *reinterpret_cast<const i32x4 *>(base + wrow + j * 32 * BK);
     };
-    auto multiply = [&](int k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[k][j], xf[k][i], acc[i][j], 0, 0, 0);
-    };
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * (LX + LW)) : "memory");
     barrier();
     read(0, 0);
     int slot = 0, ahead = NS - 1;
-    for (int kt = 0; kt < kts; ++kt) {
-        read(slot, 1);
-        __builtin_amdgcn_sched_barrier(0);                   // in this order: the reads return while the products run
-        multiply(0);
-        __builtin_amdgcn_sched_barrier(0);
+    auto turn = [&](int kt, int f) {
         slot = slot + 1 == NS ? 0 : slot + 1;
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 3) * (LX + LW)) : "memory");
-        barrier();                                           // stage kt + 1 is there, and nobody reads kt - 1 any more
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 3) * 3) : "memory");
+        barrier();                                           // step kt + 1 is there, and nobody reads kt - 1 any more
         fetch(kt + NS - 1, ahead);
         ahead = ahead + 1 == NS ? 0 : ahead + 1;
-        read(slot, 0);                                       // behind the last stage: zeros, multiplied by nobody
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(1);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    __builtin_amdgcn_s_waitcnt(0x0f70);                      // the zeros past the end are in LDS: the launch's memory is its own again
-    // residual: sixteen bytes in a row of the values' own order, exchanged between the halves as the values are; the next block's on their way
-    const bool whole = a.R && !(a.ldr & 7) && !((uintptr_t)a.R & 15) && n0 + BN <= a.N;
-    uint4 next[2];
-    auto residual = [&](int i, int j) {
-        const int li = (wm * 4 + i) * 32 + r;
-        const h16 *R = (const h16 *)a.R + (row0 + (li < rows ? li : 0)) * a.ldr + n0 + (wn * 4 + j) * 32 + hi * 8;
-        next[0] = *reinterpret_cast<const uint4 *>(R);
-        next[1] = *reinterpret_cast<const uint4 *>(R + 16);
-    };
-    if (whole) residual(0, 0);
+        read(slot, f ^ 1);                                   // behind the last step: zeros, multiplied by nobody
+        __builtin_amdgcn_sched_barrier(0);                   // in this order: the reads return while the products run
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int li = (wm * 4 + i) * 32 + r;                // row inside the tile
-        const bool there = li < rows;
-        const int64_t row = row0 + li;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[f][j], xf[f][i], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int kt = 0;
+    for (; kt + 1 < kts; kt += 2) { turn(kt, 0); turn(kt + 1, 1); }
+    if (kt < kts) turn(kt, 0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // the zeros past the end are in LDS: the launch's memory is its own again
+    // Whole features, rows that start on 16 bytes: stores and residual through buffers that end behind the last row.  The residual comes sixteen
+    // bytes in a row, as the values leave, and is exchanged between the halves as they are.
+    if (in_line && n0 + BN <= a.N) {
+        const auto cr = __builtin_amdgcn_make_buffer_rsrc((void *)((h16 *)a.C + uniform(row0 * a.ldc + n0)), 0,
+                                                          __builtin_amdgcn_readfirstlane(((rows - 1) * (int)a.ldc + BN) * 2), 0x00020000);
+        const auto rr = __builtin_amdgcn_make_buffer_rsrc((void *)((const h16 *)a.R + uniform(row0 * a.ldr + n0)), 0,
+                                                          a.R ? __builtin_amdgcn_readfirstlane(((rows - 1) * (int)a.ldr + BN) * 2) : 0, 0x00020000);
+        int co[2], ro[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int l = (wm * 2 + i) * 32 + r, col = (wn * 128 + hi * 8) * 2;
+            co[i] = l < rows ? l * (int)a.ldc * 2 + col : 0x7fff0000;
+            ro[i] = l < rows ? l * (int)a.ldr * 2 + col : 0x7fff0000;
+        }
+        i32x4 res[2][2][2];
+        auto residual = [&](int j) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) res[j & 1][i][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, ro[i] + j * 64 + h * 32, 0, 0));
+        };
+        if (a.R) residual(0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            uint32_t w[8];
-            uint32_t rw[8];
-            if (whole) {
+            if (a.R && j < 3) residual(j + 1);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const auto x = __builtin_amdgcn_permlane32_swap(next[h].x, next[h].z, false, false), y = __builtin_amdgcn_permlane32_swap(next[h].y, next[h].w, false, false);
-                    rw[4 * h] = x[0]; rw[4 * h + 1] = y[0]; rw[4 * h + 2] = x[1]; rw[4 * h + 3] = y[1];
+            for (int h = 0; h < 2; ++h) {
+                f32x4 s[2], bv[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int nl = (wn * 4 + j) * 32 + (2 * h + q) * 8 + hi * 4;
+                    s[q] = *reinterpret_cast<const f32x4 *>(sws + nl);
+                    bv[q] = *reinterpret_cast<const f32x4 *>(bs + nl);
                 }
-                if (i * 4 + j < 15) residual(j < 3 ? i : i + 1, j < 3 ? j + 1 : 0);
-            }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int nl = (wn * 4 + j) * 32 + q * 8 + hi * 4, n = n0 + nl;
-                const f32x4 s = *reinterpret_cast<const f32x4 *>(sws + nl), bv = *reinterpret_cast<const f32x4 *>(bs + nl);
-                f32x4 z;
+                for (int i = 0; i < 2; ++i) {
+                    f32x4 z[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[e] = activate<h16>(ACT, fmaf((float)acc[i][j][q * 4 + e] * sa[i], s[e], bv[e]));
-                if (whole) {
-                    const h16x4 rv = __builtin_bit_cast(h16x4, make_uint2(rw[2 * q], rw[2 * q + 1]));
+                    for (int q = 0; q < 2; ++q)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[e] += (float)rv[e];
-                } else if (a.R && there) {
-                    const f32x4 rv = four((const h16 *)a.R + row * a.ldr, n, a.N);
+                        for (int e = 0; e < 4; ++e) z[q][e] = activate<h16>(ACT, fmaf((float)acc[i][j][(2 * h + q) * 4 + e] * sa[i], s[q][e], bv[q][e]));
+                    if (a.R) {
+                        const i32x4 v = res[j & 1][i][h];
+                        const auto x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false), y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[e] += rv[e];
+                        for (int q = 0; q < 2; ++q) {
+                            const h16x4 rv = __builtin_bit_cast(h16x4, make_uint2(x[q], y[q]));
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[q][e] += (float)rv[e];
+                        }
+                    }
+                    const auto x = __builtin_amdgcn_permlane32_swap(pack2_h16(z[0][0], z[0][1]), pack2_h16(z[1][0], z[1][1]), false, false);
+                    const auto y = __builtin_amdgcn_permlane32_swap(pack2_h16(z[0][2], z[0][3]), pack2_h16(z[1][2], z[1][3]), false, false);
+                    __builtin_amdgcn_raw_buffer_store_b128(i32x4{(int)x[0], (int)y[0], (int)x[1], (int)y[1]}, cr, co[i] + j * 64 + h * 32, 0, 0);
                 }
-                w[2 * q] = pack2_h16(z[0], z[1]);
-                w[2 * q + 1] = pack2_h16(z[2], z[3]);
             }
-            store_halves(a, w, row, n0 + (wn * 4 + j) * 32, hi, there);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int li = (wm * 2 + i) * 32 + r;            // row inside the tile
+            const bool there = li < rows;
+            const int64_t row = row0 + li;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t w[8];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int nl = (wn * 4 + j) * 32 + q * 8 + hi * 4;
+                    const f32x4 s = *reinterpret_cast<const f32x4 *>(sws + nl), bv = *reinterpret_cast<const f32x4 *>(bs + nl);
+                    f32x4 z;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[e] = activate<h16>(ACT, fmaf((float)acc[i][j][q * 4 + e] * sa[i], s[e], bv[e]));
+                    if (a.R && there) {
+                        const f32x4 rv = four((const h16 *)a.R + row * a.ldr, n0 + nl, a.N);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[e] += rv[e];
+                    }
+                    w[2 * q] = pack2_h16(z[0], z[1]);
+                    w[2 * q + 1] = pack2_h16(z[2], z[3]);
+                }
+                store_halves(a, w, row, n0 + (wn * 4 + j) * 32, hi, there);
+            }
         }
     }
 #endif
@@ -453,50 +481,53 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
     i32x4 w[TF][KS];
     auto weights = [&](int p) {
         const int8_t *W = a.W + p * a.w_pstride;
+        const int feats = a.N - n0 < TF * 32 ? a.N - n0 : TF * 32;
+        const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)(W + uniform((int64_t)n0 * a.ldw)), 0,
+                                                          __builtin_amdgcn_readfirstlane(works ? (feats - 1) * (int)a.ldw + a.K : 0), 0x00020000);
 #pragma unroll
-        for (int j = 0; j < TF; ++j) {
-            const int n = n0 + j * 32 + r;
+        for (int j = 0; j < TF; ++j)
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                w[j][k] = i32x4{0, 0, 0, 0};
-                if (works && n < a.N && (k * 2 + hi) * 16 < a.K) w[j][k] = *reinterpret_cast<const i32x4 *>(W + n * a.ldw + (k * 2 + hi) * 16);
+                const int c = (k * 2 + hi) * 16;
+                w[j][k] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, c < a.K ? (j * 32 + r) * (int)a.ldw + c : 0x7ffffff0, 0, 0));
             }
-        }
         for (int i = threadIdx.x; i < NF; i += 256) {
             const int n = f0 + i;
-            sws[i] = n < a.N ? a.sw[p * a.sw_pstride + n] : 0.f;
-            bs[i] = n >= a.N || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n];
+            sws[i] = n < a.N ? plain_nan(a.sw[p * a.sw_pstride + n]) : 0.f;
+            bs[i] = n >= a.N || !a.bias ? 0.f : plain_nan(a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n]);
         }
     };
-    i32x16 done[TF];                                         // the last step's sums, its rows and what belongs to them
+    // the last step's rows and what belongs to them
     Step prev{0, 0, 0};
     float sa = 0.f, cr = 0.f;
     [[maybe_unused]] Largest<ACT> most;
     [[maybe_unused]] uint32_t o[4];
-    f32x4 sv, bv;
-    auto scales = [&](int j, int q) {
-        const int nl = (wave * TF + j) * 32 + q * 8 + hi * 4;
-        sv = *reinterpret_cast<const f32x4 *>(sws + nl);
-        bv = *reinterpret_cast<const f32x4 *>(bs + nl);
+    f32x4 sv[2], bv[2];
+    auto scales = [&](int g) {                               // of the g-th four features of a wave
+        const int nl = wave * TF * 32 + g * 8 + hi * 4;
+        sv[g & 1] = *reinterpret_cast<const f32x4 *>(sws + nl);
+        bv[g & 1] = *reinterpret_cast<const f32x4 *>(bs + nl);
     };
-    auto quad = [&](int j, int q) {                          // four features of the last step's rows
-        f32x4 z;
+    [[maybe_unused]] uint32_t c4[4];
+    i32x16 done[TF];                                         // the sums of the step before
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = fmaf((float)done[j][q * 4 + e] * sa, sv[e], bv[e]);
-        if constexpr (MODE == I8_AMAX) {
+    for (int j = 0; j < TF; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) most.take(z[e]);
-        } else {
-            int c[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) c[e] = (int)__builtin_rintf(activate<h16>(ACT, z[e]) * cr);
-            o[q] = pack4_i8(c[0], c[1], c[2], c[3]);
-            if (q == 3) {
+        for (int e = 0; e < 16; ++e) done[j][e] = 0;
+    auto value = [&](int v) {                                // the v-th of a lane's values of the last step
+        const int j = v / 16, g = v / 4, q = g % 4, e = v % 4;
+        if (e == 0 && g + 1 < 4 * TF) scales(g + 1);
+        const float z = fmaf((float)done[j][v % 16] * sa, sv[g & 1][e], bv[g & 1][e]);
+        if constexpr (MODE == I8_AMAX) most.take(z);
+        else {
+            // rounded by the addition of 1.5 2^23: the code is the low byte of the sum, 0 where it is NaN
+            c4[e] = __float_as_uint(fmaf(ACT == ACT_RELU ? fmaxf(z, 0.f) : activate<h16>(ACT, z), cr, 12582912.f));
+            if (e == 3) o[q] = __builtin_amdgcn_perm(c4[1], c4[0], 0x0c0c0400u) | __builtin_amdgcn_perm(c4[3], c4[2], 0x04000c0cu);
+            if (e == 3 && q == 3) {
                 const auto x = __builtin_amdgcn_permlane32_swap(o[0], o[2], false, false), y = __builtin_amdgcn_permlane32_swap(o[1], o[3], false, false);
                 const int n = n0 + j * 32 + hi * 16;
-                const auto cr_ = __builtin_amdgcn_make_buffer_rsrc((void *)(a.codes + uniform(prev.row0 * a.N)), 0, prev.rows * a.N, 0x00020000);
-                const bool in = works && r < prev.rows && n < a.N;
-                __builtin_amdgcn_raw_buffer_store_b128(i32x4{(int)x[0], (int)x[1], (int)y[0], (int)y[1]}, cr_, in ? r * a.N + n : 0x7ffffff0, 0, 0);
+                const auto cr_ = __builtin_amdgcn_make_buffer_rsrc((void *)(a.codes + uniform(prev.row0 * a.N)), 0, __builtin_amdgcn_readfirstlane(prev.rows * a.N), 0x00020000);
+                __builtin_amdgcn_raw_buffer_store_b128(i32x4{(int)x[0], (int)x[1], (int)y[0], (int)y[1]}, cr_, works && n < a.N ? r * a.N + n : 0x7ffffff0, 0, 0);
             }
         }
     };
@@ -504,36 +535,23 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
         if constexpr (MODE == I8_AMAX) {
             const uint32_t m = most.bits();
             const auto x = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-            const auto pr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.part + uniform((group * per + wave) * all_rows + prev.row0)), 0, prev.rows * 4, 0x00020000);
+            const auto pr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.part + uniform((group * per + wave) * all_rows + prev.row0)), 0,
+                                                              __builtin_amdgcn_readfirstlane(prev.rows * 4), 0x00020000);
             __builtin_amdgcn_raw_buffer_store_b32((int)(x[0] > x[1] ? x[0] : x[1]), pr, works && hi == 0 ? r * 4 : 0x7ffffff0, 0, 0);
             most = Largest<ACT>();
         }
     };
+    auto flush = [&]() {
+        scales(0);
 #pragma unroll
-    for (int j = 0; j < TF; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) done[j][e] = 0;
-    for (int s = 0; s < NS - 1; ++s) fetch(first + s, s);
-    int slot = 0, ahead = NS - 1, p_at = -1;
-    for (int s = first; s < last; ++s) {
-        const Step st = step_of(s);
-        const int p = a.P > 1 && a.pattern_id ? a.pattern_id[st.b] : 0;
-        if (p != p_at) {
-            if (p_at >= 0) {                                 // the last pattern's scales are still wanted
-#pragma unroll
-                for (int j = 0; j < TF; ++j)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) { scales(j, q); quad(j, q); }
-                finish();
-                prev.rows = 0;
-                barrier();
-            }
-            weights(p);
-            p_at = p;
-            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0), as the compiler understands it: it would wait for the weights at their use
-        }
+        for (int v = 0; v < 16 * TF; ++v) value(v);
+        finish();
+    };
+    int slot = 0, ahead = NS - 1;
+    // step s, while the one before is finished
+    auto turn = [&](int s) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(E + (NS - 2) * (F + E) < 63 ? E + (NS - 2) * (F + E) : 63) : "memory");
-        barrier();                                       // step s is there, and nobody reads the one before it any more
+        barrier();                                           // step s is there, and nobody reads the one before it any more
         fetch(s + NS - 1, ahead);
         const char *xs = lds + slot * SLOT + r * RB;
         const float *xsc = reinterpret_cast<const float *>(lds + slot * SLOT + TILE);
@@ -546,36 +564,49 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
             for (int e = 0; e < 16; ++e) acc[j][e] = 0;
         i32x4 xf[2];
         xf[0] = *reinterpret_cast<const i32x4 *>(xs + (hi ^ (r & 7)) * 16);
-        scales(0, 0);
+        scales(0);
+        __builtin_amdgcn_sched_barrier(0);
+        // A wave issues in order: vector instructions behind the last product of a step of K overlap with that one alone (a step took 4250 clocks for
+        // 2304 of products so).  They are spread: between two products stands a value's share, and nothing moves across.
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             if (k + 1 < KS) xf[(k + 1) & 1] = *reinterpret_cast<const i32x4 *>(xs + (((k + 1) * 2 + hi) ^ (r & 7)) * 16);
 #pragma unroll
-            for (int j = 0; j < TF; ++j) acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j][k], xf[k & 1], acc[j], 0, 0, 0);
-            // 4 TF quads over the KS steps
+            for (int j = 0; j < TF; ++j) {
+                acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j][k], xf[k & 1], acc[j], 0, 0, 0);
+                constexpr int SLOTS = KS * TF;
 #pragma unroll
-            for (int q = 4 * TF * k / KS; q < 4 * TF * (k + 1) / KS; ++q) {
-                quad(q / 4, q % 4);
-                if (q + 1 < 4 * TF) scales((q + 1) / 4, (q + 1) % 4);
+                for (int v = 16 * TF * (k * TF + j) / SLOTS; v < 16 * TF * (k * TF + j + 1) / SLOTS; ++v) value(v);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
         }
         finish();
 #pragma unroll
         for (int j = 0; j < TF; ++j) done[j] = acc[j];
-        prev = st;
+        prev = step_of(s);
         sa = sa_now;
         if constexpr (MODE == I8_CODES)                      // below 2^-100 a row counts as zeros: 127 / amax would overflow
             cr = __float_as_uint(top_now) < 0x7f800000u && top_now >= 0x1p-100f ? 127.0f / top_now : 0.f;
         slot = slot + 1 == NS ? 0 : slot + 1;
         ahead = ahead + 1 == NS ? 0 : ahead + 1;
+    };
+    for (int s = 0; s < NS - 1; ++s) fetch(first + s, s);
+    for (int s = first; s < last;) {
+        // a run of steps of one pattern
+        const int b0 = step_of(s).b, p = a.P > 1 && a.pattern_id ? __builtin_amdgcn_readfirstlane(a.pattern_id[b0]) : 0;
+        int end = last;
+        if (a.P > 1 && a.pattern_id)
+            for (int b = b0 + 1; (int64_t)b * steps_l < last; ++b)
+                if (__builtin_amdgcn_readfirstlane(a.pattern_id[b]) != p) { end = b * steps_l; break; }
+        if (s > first) barrier();                            // the last pattern's scales have been read
+        weights(p);
+        __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0), as the compiler understands it: it would wait for the weights at their use
+        barrier();
+        for (; s < end; ++s) turn(s);
+        flush();
+        prev.rows = 0;                                       // finished: the next turn stores nothing
     }
-#pragma unroll
-    for (int j = 0; j < TF; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) { scales(j, q); quad(j, q); }
-    finish();
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the zeros past the end are in LDS: the launch's memory is its own again
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // the zeros past the end are in LDS: the launch's memory is its own again
 #endif
 }
 
@@ -616,15 +647,15 @@ int32_t launch_act(const GemmI8 &a, hipStream_t st)
     return fail(SF_ERR_UNSUPPORTED, "gemm_i8: this mode takes an activation");
 }
 
-// Tiles: 256 x 256 where whole rounds of one per compute unit hold at least two thirds of values (and for 16-bit values alone), 128 x 128 where they give every
+// Tiles: 128 x 256 where whole rounds of two per compute unit hold at least two thirds of values (and for 16-bit values alone), 128 x 128 where they give every
 // compute unit one, 64 x 64 or 32 x 64 with more stages ahead where they do not
 enum Tile { WIDE, BIG, MIDDLE, SMALL };
 Tile tile_of(const GemmI8 &a, bool values)
 {
     const int64_t samples = a.P > 1 ? a.B : 1, L = a.P > 1 ? a.L : a.B * a.L;
     auto tiles = [&](int m, int n) { return samples * ((L + m - 1) / m) * ((a.N + n - 1) / n); };
-    const int64_t rounds = (tiles(256, 256) + 255) / 256;
-    if (values && 3 * samples * L * a.N >= 2 * rounds * 256 * 65536) return WIDE;
+    const int64_t rounds = (tiles(128, 256) + 511) / 512;
+    if (values && 3 * samples * L * a.N >= 2 * rounds * 512 * 32768) return WIDE;
     return tiles(128, 128) >= 256 ? BIG : tiles(64, 64) >= 256 ? MIDDLE : SMALL;
 }
 
@@ -672,16 +703,17 @@ template <int ACT>
 int32_t launch_wide(const GemmI8 &a, hipStream_t st)
 {
     auto kern = gemm_i8_wide_kernel<ACT>;
-    constexpr int LDS = 4 * 512 * 64;
+    constexpr int LDS = 6 * 384 * 32;
     static std::atomic<bool> attr_set{false};     // setting the attribute twice is harmless
     if (!attr_set) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
             return fail(SF_ERR_HIP, "gemm_i8: cannot reserve LDS");
         attr_set = true;
     }
-    const int64_t tiles_l = (a.L + 255) / 256, tiles_n = (a.N + 255) / 256, grid = a.B * tiles_l * tiles_n;
+    const int64_t tiles_l = (a.L + 127) / 128, tiles_n = (a.N + 255) / 256, grid = a.B * tiles_l * tiles_n;
     if (grid > 0x7fffffff) return fail(SF_ERR_SHAPE, "gemm_i8: too many tiles");
-    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), LDS, st, a, (int)tiles_n, (int)tiles_l);
+    const bool in_line = a.ldc % 8 == 0 && !((uintptr_t)a.C & 15) && (!a.R || (a.ldr % 8 == 0 && !((uintptr_t)a.R & 15))) && a.ldc < 1 << 21 && a.ldr < 1 << 21;
+    hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), LDS, st, a, (int)tiles_n, (int)tiles_l, (int)in_line);
     return check_launch("gemm_i8");
 }
 template <int MODE, class TC>
