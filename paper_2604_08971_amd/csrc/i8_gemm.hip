@@ -254,15 +254,17 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
 #endif
 }
 
-// Many rows and features: 128 x 256 values a workgroup, 64 x 128 a wave (six fragment reads for eight products), two workgroups per compute unit, of
-// which one finishes its tile while the other multiplies.  K in steps of 32 bytes, six of them in LDS, four on their way: 96 KB a compute unit, what the
-// latency of memory wants (256 x 256 values with 64 KB on their way took 2100 clocks for 1024 of products).  Fragments are read one step ahead.
+// Many rows and features: 256 x 256 values a workgroup, 128 x 128 a wave, one wave per SIMD.  A wave then reads eight fragments for sixteen products
+// and the LDS keeps ahead of the matrix cores (1536 of 2048 clocks per stage, with its writes; tiles of 128 x 128 need 1536 of 1024 and took 181 us for
+// 65 536 x 768 with K 2176).  Stages of 128 bytes of K - whole lines: with stages of 64 or 32 bytes the fetches were what took the time, 173 and 228 us.
+// Fragments are read one step of 32 bytes ahead, across the stages: the wait for the next one stands before a stage's last step.
 template <int ACT>
-__global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int BM = 128, BN = 256, BK = 32, NS = 6, STAGE = (BM + BN) * BK;
-    extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][rows, features][32]
+    constexpr int BM = 256, BN = 256, BK = 128, NS = 2, STAGE = (BM + BN) * BK;
+    extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][rows, features][128]
     __shared__ __attribute__((aligned(16))) float sws[BN], bs[BN];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, hi = lane >> 5;
     const int wm = wave >> 1, wn = wave & 1, kts = (a.K + BK - 1) / BK;
@@ -276,16 +278,18 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tile
     const auto ar = __builtin_amdgcn_make_buffer_rsrc((void *)(a.A + uniform(row0 * a.lda)), 0, __builtin_amdgcn_readfirstlane((rows - 1) * (int)a.lda + a.K), 0x00020000);
     const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.W + uniform(p * a.w_pstride + (int64_t)n0 * a.ldw)), 0,
                                                       __builtin_amdgcn_readfirstlane((feats - 1) * (int)a.ldw + a.K), 0x00020000);
-    // piece q of a stage: row q / 2, chunk (q % 2) ^ (row / 4 % 2) of its two, so that 16 lanes of a fragment read meet no bank twice
-    const int chunk = (threadIdx.x & 1) ^ ((threadIdx.x >> 3) & 1);
-    const int xoff = (threadIdx.x >> 1) * (int)a.lda + chunk * 16, woff = (threadIdx.x >> 1) * (int)a.ldw + chunk * 16, wstep = 128 * (int)a.ldw;
+    // piece q of a stage: row q / 8, chunk (q % 8) ^ (row % 8) of its eight, so that 16 lanes of a fragment read meet no bank twice
+    const int chunk = (threadIdx.x & 7) ^ ((threadIdx.x >> 3) & 7);
+    const int xoff = (threadIdx.x >> 3) * (int)a.lda + chunk * 16, woff = (threadIdx.x >> 3) * (int)a.ldw + chunk * 16;
+    const int xstep = 32 * (int)a.lda, wstep = 32 * (int)a.ldw;
     auto fetch = [&](int kt, int s) {                        // past the last one: zeros
         char *base = lds + s * STAGE + wave * 1024;
         const bool in = kt * BK + chunk * 16 < a.K;
-        const int xo = in ? xoff + kt * BK : 0x7ffffff0, wo = in ? woff + kt * BK : 0x7ffffff0 - wstep;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)base, 16, xo, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK), 16, wo, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK + 4096), 16, wo + wstep, 0, 0, 0);
+        const int xo = in ? xoff + kt * BK : 0x7ffffff0 - 8 * xstep, wo = in ? woff + kt * BK : 0x7ffffff0 - 8 * wstep;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(base + j * 4096), 16, xo + j * xstep, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK + j * 4096), 16, wo + j * wstep, 0, 0, 0);
     };
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) fetch(s, s);
@@ -295,46 +299,54 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tile
         sws[threadIdx.x] = in ? a.sw[p * a.sw_pstride + n] : 0.f;
         bs[threadIdx.x] = !in || !a.bias ? 0.f : a.bias_f32 ? ((const float *)a.bias)[p * a.bias_pstride + n] : (float)((const h16 *)a.bias)[p * a.bias_pstride + n];
     }
-    float sa[2];
+    float sa[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) { const int l = (wm * 2 + i) * 32 + r; sa[i] = l < rows ? a.sa[row0 + l] : 0.f; }
+    for (int i = 0; i < 4; ++i) { const int l = (wm * 4 + i) * 32 + r; sa[i] = l < rows ? a.sa[row0 + l] : 0.f; }
     __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): from here on the compiler has nothing of its own to wait for
-    i32x16 acc[2][4];
+    i32x16 acc[4][4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    const int pos = (hi ^ ((r >> 2) & 1)) * 16, xrow = (wm * 64 + r) * BK + pos, wrow = BM * BK + (wn * 128 + r) * BK + pos;
-    i32x4 xf[2][2], wf[2][4];
-    auto read = [&](int slot, int f) {
-        const char *base = lds + slot * STAGE;
+    const int xrow = (wm * 128 + r) * BK, wrow = BM * BK + (wn * 128 + r) * BK;
+    int at[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) xf[f][i] = *reinterpret_cast<const i32x4 *>(base + xrow + i * 32 * BK);
+    for (int k = 0; k < 4; ++k) at[k] = ((k * 2 + hi) ^ (r & 7)) * 16;
+    i32x4 xf[2][4], wf[2][4];
+    auto read = [&](int slot, int k) {
+        const char *base = lds + slot * STAGE + at[k];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) wf[f][j] = *reinterpret_cast<const i32x4 *>(base + wrow + j * 32 * BK);
-    };
-    barrier();
-    read(0, 0);
-    int slot = 0, ahead = NS - 1;
-    auto turn = [&](int kt, int f) {
-        slot = slot + 1 == NS ? 0 : slot + 1;
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 3) * 3) : "memory");
-        barrier();                                           // step kt + 1 is there, and nobody reads kt - 1 any more
-        fetch(kt + NS - 1, ahead);
-        ahead = ahead + 1 == NS ? 0 : ahead + 1;
-        read(slot, f ^ 1);                                   // behind the last step: zeros, multiplied by nobody
+        for (int i = 0; i < 4; ++i) {
+            xf[k & 1][i] = *reinterpret_cast<const i32x4 *>(base + xrow + i * 32 * BK);
+            wf[k & 1][i] = *reinterpret_cast<const i32x4 *>(base + wrow + i * 32 * BK);
+        }
         __builtin_amdgcn_sched_barrier(0);                   // in this order: the reads return while the products run
+    };
+    auto multiply = [&](int k) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[f][j], xf[f][i], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[k & 1][j], xf[k & 1][i], acc[i][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    int kt = 0;
-    for (; kt + 1 < kts; kt += 2) { turn(kt, 0); turn(kt + 1, 1); }
-    if (kt < kts) turn(kt, 0);
+    barrier();
+    fetch(1, 1);
+    read(0, 0);
+    for (int kt = 0; kt < kts; ++kt) {
+        const int slot = kt & 1;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            read(slot, k + 1);
+            multiply(k);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        barrier();                                           // stage kt + 1 is there, and nobody reads kt any more
+        fetch(kt + 2, slot);
+        read(slot ^ 1, 0);                                   // behind the last stage: zeros, multiplied by nobody
+        multiply(3);
+    }
     __builtin_amdgcn_s_waitcnt(0x0f70);                      // the zeros past the end are in LDS: the launch's memory is its own again
     // Whole features, rows that start on 16 bytes: stores and residual through buffers that end behind the last row.  The residual comes sixteen
     // bytes in a row, as the values leave, and is exchanged between the halves as they are.
@@ -343,17 +355,17 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tile
                                                           __builtin_amdgcn_readfirstlane(((rows - 1) * (int)a.ldc + BN) * 2), 0x00020000);
         const auto rr = __builtin_amdgcn_make_buffer_rsrc((void *)((const h16 *)a.R + uniform(row0 * a.ldr + n0)), 0,
                                                           a.R ? __builtin_amdgcn_readfirstlane(((rows - 1) * (int)a.ldr + BN) * 2) : 0, 0x00020000);
-        int co[2], ro[2];
+        int co[4], ro[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int l = (wm * 2 + i) * 32 + r, col = (wn * 128 + hi * 8) * 2;
+        for (int i = 0; i < 4; ++i) {
+            const int l = (wm * 4 + i) * 32 + r, col = (wn * 128 + hi * 8) * 2;
             co[i] = l < rows ? l * (int)a.ldc * 2 + col : 0x7fff0000;
             ro[i] = l < rows ? l * (int)a.ldr * 2 + col : 0x7fff0000;
         }
-        i32x4 res[2][2][2];
+        i32x4 res[2][4][2];
         auto residual = [&](int j) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) res[j & 1][i][h] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, ro[i] + j * 64 + h * 32, 0, 0));
         };
@@ -371,7 +383,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tile
                     bv[q] = *reinterpret_cast<const f32x4 *>(bs + nl);
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     f32x4 z[2];
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
@@ -395,8 +407,8 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_wide_kernel(GemmI8 a, int tile
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int li = (wm * 2 + i) * 32 + r;            // row inside the tile
+        for (int i = 0; i < 4; ++i) {
+            const int li = (wm * 4 + i) * 32 + r;            // row inside the tile
             const bool there = li < rows;
             const int64_t row = row0 + li;
 #pragma unroll
@@ -647,15 +659,15 @@ int32_t launch_act(const GemmI8 &a, hipStream_t st)
     return fail(SF_ERR_UNSUPPORTED, "gemm_i8: this mode takes an activation");
 }
 
-// Tiles: 128 x 256 where whole rounds of two per compute unit hold at least two thirds of values (and for 16-bit values alone), 128 x 128 where they give every
+// Tiles: 256 x 256 where whole rounds of one per compute unit hold at least two thirds of values (and for 16-bit values alone), 128 x 128 where they give every
 // compute unit one, 64 x 64 or 32 x 64 with more stages ahead where they do not
 enum Tile { WIDE, BIG, MIDDLE, SMALL };
 Tile tile_of(const GemmI8 &a, bool values)
 {
     const int64_t samples = a.P > 1 ? a.B : 1, L = a.P > 1 ? a.L : a.B * a.L;
     auto tiles = [&](int m, int n) { return samples * ((L + m - 1) / m) * ((a.N + n - 1) / n); };
-    const int64_t rounds = (tiles(128, 256) + 511) / 512;
-    if (values && 3 * samples * L * a.N >= 2 * rounds * 512 * 32768) return WIDE;
+    const int64_t rounds = (tiles(256, 256) + 255) / 256;
+    if (values && 3 * samples * L * a.N >= 2 * rounds * 256 * 65536) return WIDE;
     return tiles(128, 128) >= 256 ? BIG : tiles(64, 64) >= 256 ? MIDDLE : SMALL;
 }
 
@@ -703,14 +715,14 @@ template <int ACT>
 int32_t launch_wide(const GemmI8 &a, hipStream_t st)
 {
     auto kern = gemm_i8_wide_kernel<ACT>;
-    constexpr int LDS = 6 * 384 * 32;
+    constexpr int LDS = 2 * 512 * 128;
     static std::atomic<bool> attr_set{false};     // setting the attribute twice is harmless
     if (!attr_set) {
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
             return fail(SF_ERR_HIP, "gemm_i8: cannot reserve LDS");
         attr_set = true;
     }
-    const int64_t tiles_l = (a.L + 127) / 128, tiles_n = (a.N + 255) / 256, grid = a.B * tiles_l * tiles_n;
+    const int64_t tiles_l = (a.L + 255) / 256, tiles_n = (a.N + 255) / 256, grid = a.B * tiles_l * tiles_n;
     if (grid > 0x7fffffff) return fail(SF_ERR_SHAPE, "gemm_i8: too many tiles");
     const bool in_line = a.ldc % 8 == 0 && !((uintptr_t)a.C & 15) && (!a.R || (a.ldr % 8 == 0 && !((uintptr_t)a.R & 15))) && a.ldc < 1 << 21 && a.ldr < 1 << 21;
     hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), LDS, st, a, (int)tiles_n, (int)tiles_l, (int)in_line);
