@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int BM = 256, BN = 256, BK = 128, NS = 2, STAGE = (BM + BN) * BK;
+    constexpr int BM = 256, BN = 256, BK = 128, STAGE = (BM + BN) * BK;
     extern __shared__ __attribute__((aligned(128))) char lds[];                    // [NS][rows, features][128]
     __shared__ __attribute__((aligned(16))) float sws[BN], bs[BN];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, hi = lane >> 5;
@@ -282,17 +282,15 @@ void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
     const int chunk = (threadIdx.x & 7) ^ ((threadIdx.x >> 3) & 7);
     const int xoff = (threadIdx.x >> 3) * (int)a.lda + chunk * 16, woff = (threadIdx.x >> 3) * (int)a.ldw + chunk * 16;
     const int xstep = 32 * (int)a.lda, wstep = 32 * (int)a.ldw;
-    auto fetch = [&](int kt, int s) {                        // past the last one: zeros
-        char *base = lds + s * STAGE + wave * 1024;
+    // the wave's j-th KB of a stage, rows (0 .. 7) and features (8 .. 15); past the last stage zeros
+    auto fetch = [&](int kt, int s, int j) {
+        char *base = lds + s * STAGE + wave * 1024 + j * 4096;
         const bool in = kt * BK + chunk * 16 < a.K;
-        const int xo = in ? xoff + kt * BK : 0x7ffffff0 - 8 * xstep, wo = in ? woff + kt * BK : 0x7ffffff0 - 8 * wstep;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(base + j * 4096), 16, xo + j * xstep, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)(base + BM * BK + j * 4096), 16, wo + j * wstep, 0, 0, 0);
+        if (j < 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)base, 16, in ? xoff + kt * BK + j * xstep : 0x7ffffff0, 0, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void *)base, 16, in ? woff + kt * BK + (j - 8) * wstep : 0x7ffffff0, 0, 0, 0);
     };
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s) fetch(s, s);
+    for (int j = 0; j < 16; ++j) fetch(0, 0, j);
     {
         const int n = n0 + threadIdx.x;
         const bool in = n < a.N;
@@ -324,28 +322,34 @@ void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
         }
         __builtin_amdgcn_sched_barrier(0);                   // in this order: the reads return while the products run
     };
-    auto multiply = [&](int k) {
+    // A fetch holds up its wave's issue for some 100 clocks where others stand before it (all sixteen in a row: 3650 clocks a stage): two of them, then
+    // four products, from j on
+    auto multiply = [&](int k, int kt, int slot, int from, int to) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[k & 1][j], xf[k & 1][i], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int f = from + i * (to - from) / 4; f < from + (i + 1) * (to - from) / 4; ++f) fetch(kt, slot, f);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     barrier();
-    fetch(1, 1);
+#pragma unroll
+    for (int j = 0; j < 6; ++j) fetch(1, 1, j);
     read(0, 0);
     for (int kt = 0; kt < kts; ++kt) {
         const int slot = kt & 1;
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            read(slot, k + 1);
-            multiply(k);
-        }
+        read(slot, 1);
+        multiply(0, kt + 1, slot ^ 1, 6, 12);
+        read(slot, 2);
+        multiply(1, kt + 1, slot ^ 1, 12, 16);
+        read(slot, 3);
+        multiply(2, 0, 0, 0, 0);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         barrier();                                           // stage kt + 1 is there, and nobody reads kt any more
-        fetch(kt + 2, slot);
         read(slot ^ 1, 0);                                   // behind the last stage: zeros, multiplied by nobody
-        multiply(3);
+        multiply(3, kt + 2, slot, 0, 6);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);                      // the zeros past the end are in LDS: the launch's memory is its own again
     // Whole features, rows that start on 16 bytes: stores and residual through buffers that end behind the last row.  The residual comes sixteen
@@ -441,8 +445,9 @@ void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
 // from LDS for every two or four products; here a row fragment serves TF of them and the features none.  The values of one step are finished (scales,
 // activation, codes) between the products of the next, into whose accumulators they do not go.  A workgroup owns a group of features and a run of
 // rows; where the run comes to a sample of another pattern the weights are fetched again.
-// Waiting: a wave's memory operations complete in order as far as vmcnt tells, and it issues the same number each step: F fetches into LDS, then E
-// stores (out of range where there is nothing to store).
+// Waiting: a wave's memory operations complete in order as far as vmcnt tells, and it issues the same number each step: F fetches into LDS and E
+// stores (out of range where there is nothing to store).  The last fetch of step s may be the last operation of the turn that issues it; NS - 2 turns
+// follow before it is waited for.
 template <int KS, int TF, int MODE, int ACT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_steps)
@@ -474,20 +479,21 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
         const int q = (j * 4 + wave) * 64 + lane, row = q / CH, chunk = (q - row * CH) ^ (row & 7);
         off[j] = chunk * 16 < a.K ? row * (int)a.lda + chunk * 16 : 0x7ffffff0;
     }
-    auto fetch = [&](int s, int slot) {
+    // the wave's j-th fetch of a step: KS / 4 KB of codes, the scales, the largest values; past the last step zeros
+    struct Aim { int64_t a, row0; int an, rows; char *base; };
+    auto aim = [&](int s, int slot) {
         const Step st = step_of(s < last ? s : last - 1);
-        const int rows = s < last ? st.rows : 0;             // past the end: zeros
-        char *base = lds + slot * SLOT;
-        const auto ar = __builtin_amdgcn_make_buffer_rsrc((void *)(a.A + uniform(st.row0 * a.lda)), 0, __builtin_amdgcn_readfirstlane(rows ? (rows - 1) * (int)a.lda + a.K : 0), 0x00020000);
-        const auto sr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.sa + uniform(st.row0)), 0, rows * 4, 0x00020000);
-#pragma unroll
-        for (int j = 0; j < KS / 4; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(base + (j * 4 + wave) * 1024), 16, off[j], 0, 0, 0);
-        // every wave brings the same 32 values (and 32 zeros): the count of its operations is what matters
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, (lds_void *)(base + TILE), 4, lane * 4, 0, 0, 0);
-        if constexpr (MODE == I8_CODES) {
-            const auto tr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.top + uniform(st.row0)), 0, rows * 4, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(tr, (lds_void *)(base + TILE + 256), 4, lane * 4, 0, 0, 0);
+        const int rows = s < last ? st.rows : 0;
+        return Aim{uniform(st.row0 * a.lda), st.row0, __builtin_amdgcn_readfirstlane(rows ? (rows - 1) * (int)a.lda + a.K : 0), rows, lds + slot * SLOT};
+    };
+    auto fetch = [&](const Aim &m, int j) {
+        if (j < KS / 4) {
+            const auto ar = __builtin_amdgcn_make_buffer_rsrc((void *)(a.A + m.a), 0, m.an, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (lds_void *)(m.base + (j * 4 + wave) * 1024), 16, off[j], 0, 0, 0);
+        } else {
+            // every wave brings the same 32 values (and 32 zeros): the count of its operations is what matters
+            const auto sr = __builtin_amdgcn_make_buffer_rsrc((void *)((j == KS / 4 ? a.sa : a.top) + m.row0), 0, __builtin_amdgcn_readfirstlane(m.rows * 4), 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, (lds_void *)(m.base + TILE + (j - KS / 4) * 256), 4, lane * 4, 0, 0, 0);
         }
     };
     i32x4 w[TF][KS];
@@ -562,9 +568,9 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
     int slot = 0, ahead = NS - 1;
     // step s, while the one before is finished
     auto turn = [&](int s) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(E + (NS - 2) * (F + E) < 63 ? E + (NS - 2) * (F + E) : 63) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * (F + E) < 63 ? (NS - 2) * (F + E) : 63) : "memory");
         barrier();                                           // step s is there, and nobody reads the one before it any more
-        fetch(s + NS - 1, ahead);
+        const Aim m = aim(s + NS - 1, ahead);
         const char *xs = lds + slot * SLOT + r * RB;
         const float *xsc = reinterpret_cast<const float *>(lds + slot * SLOT + TILE);
         const float sa_now = xsc[r];
@@ -589,6 +595,8 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
                 constexpr int SLOTS = KS * TF;
 #pragma unroll
                 for (int v = 16 * TF * (k * TF + j) / SLOTS; v < 16 * TF * (k * TF + j + 1) / SLOTS; ++v) value(v);
+#pragma unroll
+                for (int f = F * (k * TF + j) / SLOTS; f < F * (k * TF + j + 1) / SLOTS; ++f) fetch(m, f);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -602,7 +610,11 @@ void gemm_i8_held_kernel(GemmI8 a, int groups, int per, int steps_l, int total_s
         slot = slot + 1 == NS ? 0 : slot + 1;
         ahead = ahead + 1 == NS ? 0 : ahead + 1;
     };
-    for (int s = 0; s < NS - 1; ++s) fetch(first + s, s);
+    for (int s = 0; s < NS - 1; ++s) {
+        const Aim m = aim(first + s, s);
+#pragma unroll
+        for (int j = 0; j < F; ++j) fetch(m, j);
+    }
     for (int s = first; s < last;) {
         // a run of steps of one pattern
         const int b0 = step_of(s).b, p = a.P > 1 && a.pattern_id ? __builtin_amdgcn_readfirstlane(a.pattern_id[b0]) : 0;
