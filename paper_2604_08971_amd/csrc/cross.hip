@@ -107,10 +107,10 @@ __device__ __forceinline__ int tiles_of(KeyTiles<KT, MASK> &t, const uint8_t *va
 // ------------------------------------------------------------------------------------------------- 16-bit models
 // WQ waves along the rows (QB blocks of 32 each), WK along the keys
 template <int DH, int WQ, int WK, int QB, bool MASK>
-__global__ __launch_bounds__(WQ *WK * 64, QB == 2 || WK == 1 ? 2 : 1) void cross_kernel(CrossArgs a)
+__global__ __launch_bounds__(WQ *WK * 64, 2) void cross_kernel(CrossArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int KT = DH == 128 && WK == 4 ? 32 : 64, RB = DH * 2, CH = DH / 8;       // keys of a tile, bytes and 16-byte chunks of a row
+    constexpr int KT = WK == 4 ? 32 : 64, RB = DH * 2, CH = DH / 8;       // keys of a tile, bytes and 16-byte chunks of a row
     constexpr int TILE = KT * RB, STAGE = WK * 2 * TILE, PIECES = TILE / 1024, ROWS = WQ * QB * 32;
     constexpr int JOIN = WK > 1 ? WK * 32 * (DH + 2) * 4 : 0;
     __shared__ __attribute__((aligned(128))) char lds[2 * STAGE > JOIN ? 2 * STAGE : JOIN];
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(WQ *WK * 64, QB == 2 || WK == 1 ? 2 : 1) void cross
 #pragma unroll
                         for (int e = 0; e < 16; ++e) o[qb][d][e] *= f;
                 }
-                const float off = LIFT - m[qb];
+                const float off = LIFT - (m[qb] == -INFINITY ? 0.f : m[qb]);    // all scores so far are -inf: weights of 0
 #pragma unroll
                 for (int sub = 0; sub < KT / 32; ++sub)
 #pragma unroll
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void cross_f32_kernel(CrossArgs a)
             l *= f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                sc[e] = __builtin_amdgcn_exp2f((sc[e] - m) * c);
+                sc[e] = __builtin_amdgcn_exp2f((sc[e] - (m == -INFINITY ? 0.f : m)) * c);       // all scores so far are -inf: weights of 0
                 l += sc[e];
             }
 #pragma unroll
@@ -500,28 +500,66 @@ __global__ __launch_bounds__(256) void cross_f32_kernel(CrossArgs a)
     if (a.splits > 1 && hi == 0) *reinterpret_cast<float2 *>(a.ml + row * 2) = make_float2(M, L);
 }
 
-// O of a row from its key ranges: sums of exp2(m_s - M) parts over that of the weights.  A thread per four dims.
+// O of a row from its key ranges: sums of exp2(m_s - M) parts over that of the weights.  A thread takes four dims and up to JOIN_RANGES ranges, whose
+// loads are all in flight at once; `groups` threads along the ranges join in LDS.
+constexpr int JOIN_RANGES = 8;
 template <class T>
-__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a)
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a, int groups)
 {
-    const int64_t all_rows = (int64_t)a.B * a.nH * a.Lq, x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int per = a.dh / 4;
-    const int64_t row = x / per;
-    if (row >= all_rows) return;
-    const int d = (int)(x % per) * 4, h = (int)(row / a.Lq % a.nH), q = (int)(row % a.Lq);
+    __shared__ f32x4 sums[256];
+    __shared__ float2 mls[256];
+    const int64_t all_rows = (int64_t)a.B * a.nH * a.Lq;
+    const int per = a.dh / 4, team = per * groups, rows = 256 / team, t = threadIdx.x % team, d = t % per * 4, y = t / per;
+    const int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / team;
+    const bool in = (int)threadIdx.x < rows * team && row < all_rows;
+    const int h = (int)(row / a.Lq % a.nH), q = (int)(row % a.Lq);
     const int64_t b = row / ((int64_t)a.nH * a.Lq);
-    const int g = a.head_group[(a.pattern_id ? (int64_t)a.pattern_id[b] * a.nH : 0) + h];
-    if (g < 0 || g >= a.nG) return;                          // a head that is not computed
-    float M = -INFINITY, L = 0.f;
-    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.ml[(s * all_rows + row) * 2]);
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float ms = a.ml[(s * all_rows + row) * 2], f = ms == M ? 1.f : __builtin_amdgcn_exp2f(ms - M);
-        L = fmaf(f, a.ml[(s * all_rows + row) * 2 + 1], L);
-        const f32x4 p = *reinterpret_cast<const f32x4 *>(a.part + (s * all_rows + row) * a.dh + d);
+    int g = -1;
+    if (in) g = a.head_group[(a.pattern_id ? (int64_t)a.pattern_id[b] * a.nH : 0) + h];
+    const bool computed = g >= 0 && g < a.nG;                // otherwise its parts were not written
+    float2 ml[JOIN_RANGES];
+    f32x4 p[JOIN_RANGES], v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(f, p[e], v[e]);
+    for (int i = 0; i < JOIN_RANGES; ++i) {
+        const int s = y + i * groups;
+        ml[i] = make_float2(-INFINITY, 0.f);
+        p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (computed && s < a.splits) {
+            ml[i] = *reinterpret_cast<const float2 *>(a.ml + (s * all_rows + row) * 2);
+            p[i] = *reinterpret_cast<const f32x4 *>(a.part + (s * all_rows + row) * a.dh + d);
+        }
     }
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < JOIN_RANGES; ++i) M = fmaxf(M, ml[i].x);
+#pragma unroll
+    for (int i = 0; i < JOIN_RANGES; ++i) {
+        const float f = ml[i].x == M ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - M);
+        L = fmaf(f, ml[i].y, L);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(f, p[i][e], v[e]);
+    }
+    if (groups > 1) {
+        mls[threadIdx.x] = make_float2(M, L);
+        sums[threadIdx.x] = v;
+        __syncthreads();
+        if (y) return;
+        const float own = M;
+        for (int k = 1; k < groups; ++k) M = fmaxf(M, mls[threadIdx.x + k * per].x);
+        const float f0 = own == M ? 1.f : __builtin_amdgcn_exp2f(own - M);
+        L *= f0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= f0;
+        for (int k = 1; k < groups; ++k) {
+            const float2 o = mls[threadIdx.x + k * per];
+            const f32x4 w = sums[threadIdx.x + k * per];
+            const float f = o.x == M ? 1.f : __builtin_amdgcn_exp2f(o.x - M);
+            L = fmaf(f, o.y, L);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(f, w[e], v[e]);
+        }
+    }
+    if (!computed) return;
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     T *out = (T *)a.O + (b * a.Lq + q) * a.ldo + (int64_t)h * a.dh + d;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(out) = make_uint2(pack2_h16(v[0] * inv, v[1] * inv), pack2_h16(v[2] * inv, v[3] * inv));
@@ -542,7 +580,7 @@ CrossPlan cross_plan(const Dims &D, int64_t Lk, int nH, int nG)
     p.wq = 4; p.wk = 1; p.qb = 1;
     if (mean <= 32) { p.wq = 1; p.wk = 4; }
     else if (half && D.dh <= 64 && mean >= 256 && rows / 256 * D.B >= 512) p.qb = 2;
-    p.kt = half ? (D.dh == 128 && p.wk == 4 ? 32 : 64) : 32;
+    p.kt = half && p.wk == 1 ? 64 : 32;
     const int own = p.wq * p.qb * 32;
     p.runs = (int)(rows / own) + nG;                          // at least the runs of all groups, whatever the heads' map
     const int64_t blocks = (int64_t)D.B * ((rows + own - 1) / own > nG ? (rows + own - 1) / own : nG);
@@ -657,10 +695,10 @@ extern "C" int32_t sf_cross_gqa_forward(const sf_desc *desc, int32_t nH, int32_t
     else if (D.dh == 64) launch_dh<64>(a, p, st);
     else launch_dh<128>(a, p, st);
     if (p.splits > 1) {
-        const int64_t threads = (int64_t)D.B * nH * D.L * (D.dh / 4);
-        const dim3 grid((unsigned)((threads + 255) / 256));
-        if (D.dtype == SF_BF16) hipLaunchKernelGGL(cross_join_kernel<h16>, grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(cross_join_kernel<float>, grid, dim3(256), 0, st, a);
+        const int groups = (p.splits + JOIN_RANGES - 1) / JOIN_RANGES, rows = 256 / (D.dh / 4 * groups);       // at most 64 ranges, 32 threads each
+        const dim3 grid((unsigned)(((int64_t)D.B * nH * D.L + rows - 1) / rows));
+        if (D.dtype == SF_BF16) hipLaunchKernelGGL(cross_join_kernel<h16>, grid, dim3(256), 0, st, a, groups);
+        else hipLaunchKernelGGL(cross_join_kernel<float>, grid, dim3(256), 0, st, a, groups);
     }
     return check_launch("cross_gqa_forward");
 }
