@@ -34,6 +34,7 @@ struct FewMoe {
     int T, L, d, E, P, top_k, ffn_pad, Fp, act; float eps; int add_residual;
     int segs, by_slot, slices, parts;                        // pairs looked at (by_slot: those of each (token, slot), else all there are);
                                                              // workgroups of a pair (up), ranges of its channels (down)
+    int per, feats;                                          // channels of a range; features of a workgroup (down)
     int tile_rows;                                           // normalised tokens in LDS at a time
     uint64_t *route; float *weight;                          // workspace, eight slots a token: experts in bytes (255: none, or listed again in a
                                                              // later slot), weights
@@ -79,12 +80,25 @@ template <> struct Operand<float> {
 template <class T> struct Weights;
 template <> struct Weights<h16> { typedef h16x8 type; };
 template <> struct Weights<float> { typedef f32x8 type; };
-__device__ __forceinline__ h16x8 load8(const h16 *p, bool in) { return in ? *reinterpret_cast<const h16x8 *>(p) : h16x8{}; }
-__device__ __forceinline__ f32x8 load8(const float *p, bool in)
+// Loads without branches, so that they stay in flight together: what is not `in` (and all of a NULL tensor) is out of range and reads as zero
+typedef __amdgpu_buffer_rsrc_t Span;
+__device__ __forceinline__ Span span_of(const void *p, int64_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, __builtin_amdgcn_readfirstlane(p ? (int)bytes : 0), 0x00020000); }
+constexpr int NOWHERE = 0x7ff00000;
+template <class V> __device__ __forceinline__ V load16(Span s, int byte, int further)
 {
-    f32x8 o{};
-    if (in) { o.a = *reinterpret_cast<const f32x4 *>(p); o.b = *reinterpret_cast<const f32x4 *>(p + 4); }
-    return o;
+    return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(s, byte, further, 0));
+}
+// eight elements `ahead` (a constant) and `further` (the same for all lanes) behind the lane's own
+template <class T> __device__ __forceinline__ typename Weights<T>::type load8(Span s, int at, bool in, int ahead = 0, int further = 0)
+{
+    const int S = sizeof(T), byte = (in ? at * S : NOWHERE) + ahead * S;
+    if constexpr (S == 2) return load16<h16x8>(s, byte, further * S);
+    else return {load16<f32x4>(s, byte, further * S), load16<f32x4>(s, byte + 16, further * S)};
+}
+template <class T> __device__ __forceinline__ float load1(Span s, int at, bool in)
+{
+    if constexpr (sizeof(T) == 2) return (float)__builtin_bit_cast(h16, __builtin_amdgcn_raw_buffer_load_b16(s, in ? at * 2 : NOWHERE, 0, 0));
+    else return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(s, in ? at * 4 : NOWHERE, 0, 0));
 }
 
 template <class T>
@@ -94,28 +108,33 @@ __device__ __forceinline__ float activated(int act, float z)
     return sizeof(T) == 4 ? 0.5f * z * (1.0f + erff(z * 0.70710678f)) : gelu_erf(z);
 }
 
+// Pattern of a lane's token
 __device__ __forceinline__ int pattern_of(const FewMoe &a, int t)
 {
-    return a.pattern_id ? min(max(a.pattern_id[t / a.L], 0), a.P - 1) : 0;
+    const int p = __builtin_amdgcn_raw_buffer_load_b32(span_of(a.pattern_id, a.T / a.L * 4), t < a.T ? t / a.L * 4 : NOWHERE, 0, 0);
+    return min(max(p, 0), a.P - 1);
 }
 
 // The `nth` pair looked at: its number (pattern E + expert), and the (token, slot) in which the lane's token chose it or -1.  by_slot: the pair of
 // (token, slot) nth.  picks: the experts of the lane's token, a byte each.  Registers of one wave only.
-struct Pair { int seg, at; };
+struct Pair { int seg, at, expert; };
 __device__ __forceinline__ Pair find_pair(const FewMoe &a, uint64_t picks, int pattern, int nth)
 {
     const int lane = threadIdx.x & 63;
-    Pair p{nth, -1};
+    Pair p{nth, -1, 0};
     if (a.by_slot) {
         const int t = nth / a.top_k, s = nth - t * a.top_k;
         const uint64_t of = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(picks >> 32), t) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)picks, t);
         const int e = (int)(of >> (8 * s)) & 255;
-        p.seg = e == 255 ? -1 : __builtin_amdgcn_readlane(pattern, t) * a.E + e;
+        if (e == 255) return p;
+        p.seg = __builtin_amdgcn_readlane(pattern, t) * a.E + e;
     }
-    if (p.seg < 0 || pattern != p.seg / a.E) return p;
-    const uint64_t x = picks ^ (uint64_t)(p.seg % a.E) * 0x0101010101010101ull;      // a zero byte where the expert is; E <= 64: none carries into the next
+    const uint32_t e = (uint32_t)(p.seg - pattern * a.E);    // the pair's expert, where the lane's token has its pattern
+    const uint64_t x = picks ^ (uint64_t)e * 0x0101010101010101ull;                  // a zero byte where the expert is; E <= 64: none carries into the next
     const uint64_t zero = ~((((x & 0x7f7f7f7f7f7f7f7full) + 0x7f7f7f7f7f7f7f7full) | x) | 0x7f7f7f7f7f7f7f7full);
-    if (zero) p.at = lane * a.top_k + (__ffsll((unsigned long long)zero) - 1) / 8;
+    if (e < (uint32_t)a.E && zero) p.at = lane * a.top_k + (__ffsll((unsigned long long)zero) - 1) / 8;
+    const uint64_t chose = __ballot(p.at >= 0);
+    if (chose) p.expert = __builtin_amdgcn_readlane((int)e, __ffsll((unsigned long long)chose) - 1);
     return p;
 }
 // The tokens that chose the pair: a list per wave, which that wave alone writes and reads.  0: not looked at here (none, or an earlier
@@ -165,16 +184,42 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
         }
     };
     // what does not depend on the tokens is on its way first
-    const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
+    const int pattern = pattern_of(a, lane), kept = __builtin_amdgcn_raw_buffer_load_b32(span_of(a.k_ffn, a.E * 4), lane * 4, 0, 0);
+    const int S = sizeof(T);
+    const Span xs = span_of(X, (int64_t)a.T * d * S), rs = span_of(a.Wr, (int64_t)a.E * d * S), gs = span_of(a.ln_g, d * S), bs = span_of(a.ln_b, d * S);
     Eight gq[NCH], bq[NCH], wr[STEPS];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
         const int at = (lane + j * 64) * 8;
-        gq[j] = load8((const T *)a.ln_g + at, a.ln_g && at < d);
-        bq[j] = load8((const T *)a.ln_b + at, a.ln_g && at < d);
+        gq[j] = load8<T>(gs, at, at < d);
+        bq[j] = load8<T>(bs, at, at < d);
     }
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) wr[j] = load8((const T *)a.Wr + (int64_t)c * d + (wave + j * WAVES) * 32 + kq, c < a.E && (wave + j * WAVES) * 32 + kq < d);
+    for (int j = 0; j < STEPS; ++j) wr[j] = load8<T>(rs, c * d + (wave + j * WAVES) * 32 + kq, c < a.E && (wave + j * WAVES) * 32 + kq < d);
+
+    // Channels of a pair, a round: G runs of sixteen, G 16 x 16 values over the waves' K; a thread stores up to two of them for one (token, slot).
+    // Where every pair there is has its workgroups, the first round's weights are on their way while the logits are made.
+    const int nth = blockIdx.x / a.slices, g0 = blockIdx.x % a.slices * G, r = threadIdx.x & 15, ch0 = threadIdx.x >> 4;
+    constexpr int EACH = G == 1 ? 1 : G / 2;
+    int seg = nth, groups = 0;
+    Eight w[G][STEPS];
+    float bias[EACH];
+    auto fetch = [&](int g) {
+        const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane(seg) * a.Fp;
+        const Span ws = span_of((const T *)a.W1 + first * d, (int64_t)a.Fp * d * S), b1 = span_of(a.b1 ? (const T *)a.b1 + first : nullptr, a.Fp * S);
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                const int k = (wave + j * WAVES) * 32 + kq;
+                w[i][j] = load8<T>(ws, ((g + i) * 16 + c) * d + k, g + i < groups && k < d);
+            }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int ch = g * 16 + ch0 + i * 32;
+            bias[i] = load1<T>(b1, ch, ch < groups * 16);
+        }
+    };
 
     // ---- route
     const bool resident = a.T <= a.tile_rows;
@@ -188,7 +233,7 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 #pragma unroll
                 for (int j = 0; j < NCH; ++j) {
                     const int at = (lane + j * 64) * 8;
-                    next[u][j] = load8(X + (int64_t)(base + i + u * WAVES) * d + at, at < d && i + u * WAVES < rows);
+                    next[u][j] = load8<T>(xs, (base + i + u * WAVES) * d + at, at < d && i + u * WAVES < rows);
                 }
         };
         load_tokens(wave);
@@ -251,6 +296,10 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
                 }
             }
         }
+        if (!a.by_slot && base + a.tile_rows >= a.T) {
+            groups = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)) / 16;
+            fetch(g0);
+        }
         __syncthreads();
         // logits in blocks of 16 experts x 16 tokens, four blocks between two barriers
         const int tiles_e = (a.E + 15) / 16, blocks = tiles_e * ((rows + TILE_T - 1) / TILE_T);
@@ -264,7 +313,7 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
                     const int s = wave + j * WAVES;
                     if (s >= steps) break;
                     Eight w = wr[j];
-                    if (e0) w = load8((const T *)a.Wr + (int64_t)(e0 + c) * d + s * 32 + kq, e0 + c < a.E && s * 32 + kq < d);
+                    if (e0) w = load8<T>(rs, (e0 + c) * d + s * 32 + kq, e0 + c < a.E && s * 32 + kq < d);
                     float v[8];
                     const float *p = xt + (r < rows ? r : 0) * ld + s * 32 + kq;      // columns from `rows` on: another's sums, not stored
 #pragma unroll
@@ -331,34 +380,16 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     }
     const uint64_t mine_picks = lane < a.T ? picks[lane] : ~0ull;
 
-    // ---- channels of a pair
-    const int nth = blockIdx.x / a.slices;
+    // ---- the pair's channels
     const Pair pair = find_pair(a, mine_picks, pattern, nth);
     const int n_all = list_tokens(a, pair, nth, slots[wave]);
     if (!n_all) return;
-    const int seg = pair.seg, groups = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)) / 16;
-    const T *W1 = (const T *)a.W1 + (int64_t)seg * a.Fp * d, *b1 = a.b1 ? (const T *)a.b1 + (int64_t)seg * a.Fp : nullptr;
-    // a round: G runs of channels, G 16 x 16 values over the waves' K; a thread stores up to two of them for one (token, slot)
-    const int g0 = blockIdx.x % a.slices * G, r = threadIdx.x & 15, ch0 = threadIdx.x >> 4;
-    constexpr int EACH = G == 1 ? 1 : G / 2;
-    Eight w[G][STEPS];
-    float bias[EACH];
-    auto fetch = [&](int g) {
-#pragma unroll
-        for (int i = 0; i < G; ++i)
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                const int k = (wave + j * WAVES) * 32 + kq;
-                w[i][j] = load8(W1 + (int64_t)((g + i) * 16 + c) * d + k, g + i < groups && k < d);
-            }
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int ch = g * 16 + ch0 + i * 32;
-            bias[i] = b1 && ch < groups * 16 ? to_f32(b1[ch]) : 0.f;
-        }
-    };
+    if (a.by_slot) {
+        seg = pair.seg;
+        groups = width_of(a, __builtin_amdgcn_readlane(kept, pair.expert)) / 16;
+    }
     for (int t0 = 0; t0 < n_all; t0 += TILE_T) {
-        fetch(g0);
+        if (a.by_slot || t0) fetch(g0);
         const int n = n_all - t0 < TILE_T ? n_all - t0 : TILE_T;
         const int token = slots[wave][t0 + (c < n ? c : 0)] / a.top_k;        // columns from n on: another's sums, not stored
         Operand<T> x[STEPS];
@@ -371,11 +402,11 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = xt[token * ld + k + e];
             } else {                                         // normalised again, from memory
-                to_floats(load8(X + (int64_t)token * d + k, k < d), v);
+                to_floats(load8<T>(xs, token * d + k, k < d), v);
                 if (a.ln_g) {
                     float gm[8], bt[8];
-                    to_floats(load8((const T *)a.ln_g + k, k < d), gm);
-                    to_floats(load8((const T *)a.ln_b + k, k < d), bt);
+                    to_floats(load8<T>(gs, k, k < d), gm);
+                    to_floats(load8<T>(bs, k, k < d), bt);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = fmaf((v[e] - mean[token]) * rstd[token], gm[e], bt[e]);
                 }
@@ -420,90 +451,136 @@ __global__ __launch_bounds__(NT) void moe_few_up_kernel(FewMoe a)
     }
 }
 
-// Four features of all tokens.  A wave takes pairs in turn (or a range of a pair's channels) and multiplies in sixteen 4 x 4 blocks at once, four
-// features by four tokens, each over channels of its own: 16 bytes of a lane are eight channels of one feature.  The sums of the slots meet in LDS.
+// Two or four features of all tokens.  A wave takes ranges of the pairs' channels as they come and multiplies in sixteen 4 x 4 blocks at once, four
+// features by four tokens, each over channels of its own: 16 bytes of a lane are eight channels of one feature.  Every (range, slot) has its own
+// place in LDS, and the end adds them up in order.  What bounds it is how much one compute unit keeps on its way, so the features are as few as still
+// leave it one workgroup: two where d <= 512 (34 tokens, sixteen experts of d 512: 24.5 us, with four 27.5), else four.
 template <class T>
 __global__ __launch_bounds__(DOWN_WAVES * 64) void moe_few_down_kernel(FewMoe a)
 {
     extern __shared__ __attribute__((aligned(16))) float zs[];         // [parts][T k][4]
-    __shared__ short slots[DOWN_WAVES][FEW + 16];
+    __shared__ short slots[DOWN_WAVES][2][FEW];             // of this pair and of the next
+    __shared__ float weight[FEW][8];
+    __shared__ uint64_t route[FEW];
+    __shared__ int taken;
+    if (threadIdx.x == 0) taken = 0;
+    for (int i = threadIdx.x; i < a.parts * a.T * a.top_k * 4; i += DOWN_WAVES * 64) zs[i] = 0.f;      // ranges past an expert's width stay so
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q4 = lane & 3, k8 = (lane >> 2) * 8;
-    const int n0 = blockIdx.x * 4, d = a.d, all = a.T * a.top_k;
+    const int n0 = blockIdx.x * a.feats, d = a.d, all = a.T * a.top_k;
     const uint64_t picks = lane < a.T ? a.route[lane] : ~0ull;
-    const int pattern = lane < a.T ? pattern_of(a, lane) : 0, kept = lane < a.E ? a.k_ffn[lane] : 0;
-    // what the end needs: a thread's feature and token, at most 64 tokens x 4
+    const int pattern = pattern_of(a, lane), kept = __builtin_amdgcn_raw_buffer_load_b32(span_of(a.k_ffn, a.E * 4), lane * 4, 0, 0);
+    // what the end needs: a thread's feature and token, at most 64 tokens x 4, and one of the weights
     const int f = threadIdx.x & 3, t = threadIdx.x >> 2;
-    const bool ends = t < a.T && n0 + f < d;
-    float y = 0.f;
-    f32x4 wt[2] = {};
-    uint64_t slot_of = ~0ull;
-    if (ends) {
-        if (a.add_residual) y = to_f32(((const T *)a.X)[(int64_t)t * d + n0 + f]);
-        wt[0] = *reinterpret_cast<const f32x4 *>(a.weight + t * 8);
-        wt[1] = *reinterpret_cast<const f32x4 *>(a.weight + t * 8 + 4);
-        slot_of = a.route[t];
-    }
-    for (int item = wave; item < a.segs * a.parts; item += DOWN_WAVES) {
-        const int nth = item / a.parts, prt = item - nth * a.parts;
-        const Pair pair = find_pair(a, picks, pattern, nth);
-        const int n_all = list_tokens(a, pair, nth, slots[wave]);
-        if (!n_all) continue;
-        const int seg = pair.seg, width = width_of(a, __builtin_amdgcn_readlane(kept, seg % a.E)), per = (width / 64 + a.parts - 1) / a.parts * 64;
-        const int from = prt * per, to = from + per < width ? from + per : width;
-        const T *W = (const T *)a.W2T + ((int64_t)seg * d + (n0 + q4 < d ? n0 + q4 : d - 1)) * a.Fp + k8;
-        f32x4 bias = {0.f, 0.f, 0.f, 0.f};
-        if (a.b2x && prt == 0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) bias[e] = to_f32(((const T *)a.b2x)[(int64_t)seg * d + (n0 + e < d ? n0 + e : d - 1)]);
+    const bool ends = t < a.T && f < a.feats && n0 + f < d;
+    const float y = load1<T>(span_of(a.X, (int64_t)a.T * d * (int)sizeof(T)), t * d + n0 + f, ends && a.add_residual);
+    const float one = load1<float>(span_of(a.weight, a.T * 32), threadIdx.x, true);
+    // Chunks of a wave: the channels of an item, up to sixteen tokens at a time, four to a product.  The weights of the next chunk, or of the next
+    // pair's first one, take the place of this one's as they are used.
+    constexpr int TT = 4, AHEAD = sizeof(T) == 2 ? 8 : 4, CHUNK = 128 * AHEAD, TERMS = sizeof(T) == 2 ? 2 : 1;
+    struct At { int item, buf, seg, prt, n_all, t0, from, to, k; };
+    auto advance = [&](At s) {
+        if (s.k + CHUNK < s.to) { s.k += CHUNK; return s; }
+        s.k = s.from;
+        s.t0 += 16;
+        if (s.t0 < s.n_all) return s;
+        for (;;) {                                           // the next item that no wave has: which wave sums it does not matter to the sum
+            if (s.item < 0) s.item = wave;
+            else {
+                int i = 0;
+                if (lane == 0) i = atomicAdd(&taken, 1);
+                s.item = DOWN_WAVES + __builtin_amdgcn_readfirstlane(i);
+            }
+            if (s.item >= a.segs * a.parts) break;
+            int nth = s.item, prt = 0;
+            for (; nth >= a.segs; nth -= a.segs) ++prt;
+            const Pair pair = find_pair(a, picks, pattern, nth);
+            const int n_all = list_tokens(a, pair, nth, slots[wave][s.buf ^ 1]);
+            if (!n_all) continue;
+            const int width = width_of(a, __builtin_amdgcn_readlane(kept, pair.expert)), from = prt * a.per;
+            if (from >= width && prt) continue;
+            return At{s.item, s.buf ^ 1, pair.seg, prt, n_all, 0, from, from + a.per < width ? from + a.per : width, from};
         }
-        for (int t0 = 0; t0 < n_all; t0 += 16) {             // up to sixteen tokens at a time, four to a product
-            constexpr int TT = 4, AHEAD = sizeof(T) == 2 ? 8 : 4;
-            int at[TT];
+        return At{s.item, s.buf, 0, 0, 0, 0, 0, 0, 0};
+    };
+    const Span hs = span_of(a.hid, (int64_t)all * a.Fp * 4);
+    typename Weights<T>::type w[AHEAD];
+    auto fetch = [&](const At &s, int j) {
+        const Span ws = span_of((const T *)a.W2T + ((int64_t)__builtin_amdgcn_readfirstlane(s.seg) * d + n0) * a.Fp, (int64_t)(d - n0) * a.Fp * (int)sizeof(T));
+        w[j] = load8<T>(ws, q4 * a.Fp + s.k + k8, s.k + k8 < (q4 < a.feats && n0 + q4 < d ? s.to - j * 128 : 0), j * 128);
+    };
+    At cur = advance(At{-1, 0, 0, 0, 0, 0, 0, 0, 0});
 #pragma unroll
-            for (int u = 0; u < TT; ++u) at[u] = t0 + u * 4 + q4 < n_all ? slots[wave][t0 + u * 4 + q4] : -1;
-            f32x4 acc[TT];
+    for (int j = 0; j < AHEAD; ++j) fetch(cur, j);
+    int at[TT];
+    f32x4 acc[TT], bias;
+    while (cur.n_all) {
+        if (cur.k == cur.from) {
 #pragma unroll
-            for (int u = 0; u < TT; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k = from; k < to; k += 128 * AHEAD) {
-                typename Weights<T>::type w[AHEAD];
+            for (int u = 0; u < TT; ++u) {
+                at[u] = cur.t0 + u * 4 + q4 < cur.n_all ? slots[wave][cur.buf][cur.t0 + u * 4 + q4] : -1;
+                acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            const Span b2 = span_of(a.b2x ? (const T *)a.b2x + (int64_t)__builtin_amdgcn_readfirstlane(cur.seg) * d + n0 : nullptr, (d - n0) * (int)sizeof(T));
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) w[j] = load8(W + k + j * 128, k + j * 128 + k8 < to);
+            for (int e = 0; e < 4; ++e)
+                bias[e] = load1<T>(b2, e, cur.prt == 0);
+        }
+        const At next = advance(cur);
+        const int left = cur.n_all - cur.t0;
 #pragma unroll
-                for (int u = 0; u < TT; ++u) {
-                    if (t0 + u * 4 >= n_all) break;
+        for (int u = 0; u < TT; ++u) {
+            if (u * 4 >= left) break;
+            const bool last = u + 1 == TT || (u + 1) * 4 >= left;
 #pragma unroll
-                    for (int j = 0; j < AHEAD; ++j) {
-                        const bool in = at[u] >= 0 && k + j * 128 + k8 < to;
-                        const int64_t h = (int64_t)at[u] * a.Fp + k + j * 128 + k8;
-                        if constexpr (sizeof(T) == 2) {
-                            const h16x8 hi = load8((const h16 *)a.hid + h, in), lo = load8((const h16 *)a.hid + (int64_t)all * a.Fp + h, in);
+            for (int j0 = 0; j0 < AHEAD; j0 += 4) {
+                typename Weights<T>::type x[4][TERMS];       // hidden channels of four products on their way together
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int v = 0; v < TERMS; ++v) {
+                        const int k = cur.k + k8;
+                        x[j][v] = load8<T>(hs, at[u] * a.Fp + k, k < (at[u] < 0 ? 0 : cur.to - (j0 + j) * 128), (j0 + j) * 128, v * all * a.Fp);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (sizeof(T) == 2) {
 #define SF_QUARTER(x, i) __builtin_shufflevector(x, x, (i) * 4, (i) * 4 + 1, (i) * 4 + 2, (i) * 4 + 3)
-                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 0), SF_QUARTER(lo, 0), acc[u]);
-                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 1), SF_QUARTER(lo, 1), acc[u]);
-                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 0), SF_QUARTER(hi, 0), acc[u]);
-                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j], 1), SF_QUARTER(hi, 1), acc[u]);
-#undef SF_QUARTER
-                        } else {
-                            const f32x8 v = load8((const float *)a.hid + h, in);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[u] = __builtin_amdgcn_mfma_f32_4x4x1f32(w[j].a[e], v.a[e], acc[u], 0, 0, 0);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[u] = __builtin_amdgcn_mfma_f32_4x4x1f32(w[j].b[e], v.b[e], acc[u], 0, 0, 0);
+                        for (int v = TERMS - 1; v >= 0; --v) {
+                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j0 + j], 0), SF_QUARTER(x[j][v], 0), acc[u]);
+                            acc[u] = SF_MFMA_4X4(SF_QUARTER(w[j0 + j], 1), SF_QUARTER(x[j][v], 1), acc[u]);
                         }
+#undef SF_QUARTER
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[u] = __builtin_amdgcn_mfma_f32_4x4x1f32(w[j0 + j].a[e], x[j][0].a[e], acc[u], 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[u] = __builtin_amdgcn_mfma_f32_4x4x1f32(w[j0 + j].b[e], x[j][0].b[e], acc[u], 0, 0, 0);
                     }
                 }
             }
+            if (last) {
 #pragma unroll
-            for (int u = 0; u < TT; ++u) {
-                if (t0 + u * 4 >= n_all) break;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[u][e] = pair_sum<4>(pair_sum<8>(pair_sum<16>(pair_sum<32>(acc[u][e])))) + bias[e];
-                if (lane < 4 && at[u] >= 0) *reinterpret_cast<f32x4 *>(zs + (prt * all + at[u]) * 4) = acc[u];
+                for (int j = 0; j < AHEAD; ++j) fetch(next, j);
             }
         }
+        if (next.item != cur.item || next.t0 != cur.t0) {
+#pragma unroll
+            for (int u = 0; u < TT; ++u) {
+                if (u * 4 >= left) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[u][e] = pair_sum<4>(pair_sum<8>(pair_sum<16>(pair_sum<32>(acc[u][e])))) + bias[e];
+                if (lane < 4 && at[u] >= 0) *reinterpret_cast<f32x4 *>(zs + (cur.prt * all + at[u]) * 4) = acc[u];
+            }
+        }
+        cur = next;
     }
+    if (threadIdx.x < FEW * 8) weight[threadIdx.x / 8][threadIdx.x % 8] = one;
+    if (threadIdx.x < FEW) route[threadIdx.x] = picks;
     __syncthreads();
     if (!ends) return;
+    const uint64_t slot_of = route[t];
     float sum = 0.f;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
@@ -511,12 +588,12 @@ __global__ __launch_bounds__(DOWN_WAVES * 64) void moe_few_down_kernel(FewMoe a)
         if (((slot_of >> (8 * s)) & 255) == 255) continue;
         float z = 0.f;
         for (int q = 0; q < a.parts; ++q) z += zs[(q * all + t * a.top_k + s) * 4 + f];
-        sum = fmaf(wt[s / 4][s % 4], z, sum);
+        sum = fmaf(weight[t][s], z, sum);
     }
     ((T *)a.Y)[(int64_t)t * d + n0 + f] = from_f32<T>(y + sum);
 }
 
-struct FewWs { uint64_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, groups, parts; size_t bytes; };
+struct FewWs { uint64_t *route; float *weight; void *hid; int Fp, segs, by_slot, slices, groups, parts, per; size_t bytes; };
 FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
 {
     Carver c(ws);
@@ -530,7 +607,9 @@ FewWs few_ws(const Dims &D, const sf_moe_compact &m, void *ws)
     const int together = D.dtype == SF_BF16 ? 4 : 2;          // fp32 weights take twice the registers
     w.groups = w.Fp / 16 >= together * w.slices ? together : 1;
     w.slices = std::min(ceil_div(w.Fp / 16, w.groups), w.slices);
-    w.parts = std::max(1, DOWN_WAVES / w.segs);
+    // ranges of 1024 channels, where few pairs share a workgroup's waves as many as there are waves; their sums take at most 48 KB
+    w.parts = std::max(1, std::min(std::max(ceil_div(w.Fp, 1024), DOWN_WAVES / w.segs), 48 * 1024 / (pairs * 16)));
+    w.per = align_up((size_t)ceil_div(w.Fp, w.parts), 64);
     w.route = c.take<uint64_t>((size_t)T);
     w.weight = c.take<float>((size_t)T * 8);
     w.hid = c.take<float>((size_t)pairs * w.Fp);
@@ -544,6 +623,7 @@ int32_t check_few(const Dims &D, const sf_moe_compact *m)
     if (m->n_experts < 1 || m->n_experts > 64 || m->top_k < 1 || m->top_k > m->n_experts || m->top_k > 8)
         return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: needs 1 <= top_k <= min(8, n_experts), n_experts <= 64");
     if (m->k_ffn_max < 1 || m->k_ffn_max > D.F) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: k_ffn_max out of range");
+    if (m->k_ffn_max > 1 << 18) return fail(SF_ERR_SHAPE, "moe_ffn_few: at most 2^18 channels an expert");
     if (!m->k_ffn) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: k_ffn (device keep counts) missing");
     if ((int64_t)D.B * D.L > FEW) return fail(SF_ERR_SHAPE, "moe_ffn_few: at most %d tokens (sf_moe_ffn_forward takes any number)", FEW);
     if ((int64_t)D.P * m->n_experts > 4096) return fail(SF_ERR_SHAPE, "moe_ffn_few: more than 4096 (pattern, expert) pairs");
@@ -585,7 +665,7 @@ extern "C" int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_comp
     a.pattern_id = D.P > 1 ? pattern_id : nullptr; a.forced = forced_route; a.k_ffn = m->k_ffn;
     a.T = D.B * D.L; a.L = D.L; a.d = D.d; a.E = m->n_experts; a.P = D.P; a.top_k = m->top_k; a.ffn_pad = D.ffn_pad; a.Fp = w.Fp;
     a.act = D.act == SF_GELU_ERF ? ACT_GELU : ACT_RELU; a.eps = D.eps; a.add_residual = add_residual;
-    a.segs = w.segs; a.by_slot = w.by_slot; a.slices = w.slices; a.parts = w.parts;
+    a.segs = w.segs; a.by_slot = w.by_slot; a.slices = w.slices; a.parts = w.parts; a.per = w.per;
     a.route = w.route; a.weight = w.weight; a.hid = w.hid;
     a.Y = Y; a.route_out = route_out; a.weight_out = weight_out; a.logit_out = logit_out;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -602,7 +682,8 @@ extern "C" int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_comp
         attr_set[which] = true;
     }
     hipLaunchKernelGGL(kern, dim3((unsigned)(w.segs * w.slices)), dim3(NT), lds, st, a);
-    const dim3 down((unsigned)ceil_div(D.d, 4));
+    a.feats = D.d <= 2 * 256 ? 2 : 4;                        // 256 compute units
+    const dim3 down((unsigned)ceil_div(D.d, a.feats));
     const size_t zs = (size_t)w.parts * a.T * a.top_k * 4 * sizeof(float);
     if (bf) hipLaunchKernelGGL(moe_few_down_kernel<h16>, down, dim3(DOWN_WAVES * 64), zs, st, a);
     else hipLaunchKernelGGL(moe_few_down_kernel<float>, down, dim3(DOWN_WAVES * 64), zs, st, a);
