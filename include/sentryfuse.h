@@ -377,7 +377,7 @@ int32_t sf_encoder_forward_fp8(const sf_desc *desc, const sf_compact_layer *laye
  *
  * sf_linear_i8_forward: Y = act(Q(X) W^T s + bias) (+ R), the rows of X
  * quantised as they come.  X [rows, K], R and Y [rows, N] of type dtype with
- * strides ldx, ldr, ldy in elements; R may be NULL and may be Y.  sf_linear_i8: W
+ * strides ldx, ldr, ldy in elements; R may be NULL and may be Y (ldr = ldy).  sf_linear_i8: W
  * codes [N, K] (16-byte aligned, stride ldw a multiple of 16), s [N] fp32, bias
  * [N] of type dtype or NULL.  act: SF_ACT_NONE, SF_RELU, SF_GELU_ERF.  K a
  * multiple of 16, at most 65536.  Otherwise rounded once, to dtype.
@@ -770,7 +770,8 @@ int32_t sf_moe_ffn_forward(const sf_desc *desc, const sf_moe_compact *moe_host, 
  * LayerNorm output and the hidden activations stay in fp32 -, so logits, and with
  * them a choice between two almost equal experts, may differ from
  * sf_moe_ffn_forward's in the places that a 16-bit xn moves; d_model a
- * multiple of 8, at most 1024; X, Y, Wr, W1 and W2T on 16 bytes.  binary16: hidden
+ * multiple of 8, at most 1024; k_ffn_max at most 2^18; X, Y, Wr, W1, W2T, ln_g and
+ * ln_b on 16 bytes.  binary16: hidden
  * activations must fit the type, as above. */
 #define SF_MOE_FEW_TOKENS 64
 size_t sf_moe_ffn_few_workspace_bytes(const sf_desc *desc, const sf_moe_compact *moe_host);

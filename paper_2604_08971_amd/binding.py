@@ -276,10 +276,16 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _stream_of(t: torch.Tensor) -> int:
-    """The current stream, for a call on t's device: that has to be the current device, where the launches go."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise SentryFuseError(f"tensors on {t.device}, which is not the current device")
+def _stream_of(*tensors: Optional[torch.Tensor]) -> int:
+    """The current stream, for a call on these tensors: all of them have to be on the current device, where the launches go."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        at = t.get_device()
+        if at < 0 or at != (torch.cuda.current_device() if device is None else device):
+            raise SentryFuseError(f"a tensor on {t.device}, which is not the current device")
+        device = at
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -580,6 +586,12 @@ def sparse_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.
     return O, sel, score
 
 
+def _strides_of(t: torch.Tensor) -> SfStrides:
+    """As _strides4, with 0 for a dimension of one element, whose stride says nothing."""
+    assert t.dim() == 4 and t.stride(3) == 1
+    return SfStrides(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+
+
 def cross_gqa_workspace_bytes(desc: SfDesc, Lk: int, nH: int, nG: int) -> int:
     return int(lib().sf_cross_gqa_workspace_bytes(C.byref(desc), int(Lk), int(nH), int(nG)))
 
@@ -588,7 +600,7 @@ def cross_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.T
                       pattern_id: Optional[torch.Tensor] = None, key_valid: Optional[torch.Tensor] = None,
                       out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Q [B,nH,Lq,dh] over K, V [B,nG,Lk,dh] (last dimension contiguous, any other strides), desc with L = Lq;
-    head_group [n_maps,nH] int32, key_valid [B,Lk] u8.  Returns O [B,Lq,nH*dh] (out: row stride any)."""
+    head_group [n_maps,nH] int32, key_valid [B,Lk] u8.  Returns O [B,Lq,nH*dh] (out: row stride any, the same over all samples)."""
     B, nH, Lq, dh = Q.shape
     nG, Lk, dt = K.shape[1], K.shape[2], Q.dtype
     assert (desc.B, desc.L, desc.dh) == (B, Lq, dh) and dt == torch_dtype(desc.dtype) == K.dtype == V.dtype
@@ -598,13 +610,15 @@ def cross_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.T
     assert key_valid is None or (key_valid.dtype == torch.uint8 and key_valid.is_contiguous() and tuple(key_valid.shape) == (B, Lk))
     if out is None:
         out = torch.empty((B, Lq, nH * dh), dtype=dt, device=Q.device)
-    assert out.dtype == dt and tuple(out.shape) == (B, Lq, nH * dh) and out.stride(2) == 1 and (B == 1 or out.stride(0) == Lq * out.stride(1))
+    assert out.dtype == dt and tuple(out.shape) == (B, Lq, nH * dh) and out.stride(2) == 1
+    assert B == 1 or Lq == 1 or out.stride(0) == Lq * out.stride(1), "out: rows equally spaced over all samples"
+    ldo = out.stride(1) if Lq > 1 else out.stride(0) if B > 1 else nH * dh
     if ws is None:
         ws = workspace(cross_gqa_workspace_bytes(desc, Lk, nH, nG), Q.device)
-    _check(lib().sf_cross_gqa_forward(C.byref(desc), nH, nG, Lk, Q.data_ptr(), _strides4(Q), K.data_ptr(), _strides4(K), V.data_ptr(),
-                                      _strides4(V), head_group.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
-                                      None if key_valid is None else key_valid.data_ptr(), out.data_ptr(), out.stride(1), ws.data_ptr(),
-                                      ws.numel(), _stream_of(Q)), "sf_cross_gqa_forward")
+    _check(lib().sf_cross_gqa_forward(C.byref(desc), nH, nG, Lk, Q.data_ptr(), _strides_of(Q), K.data_ptr(), _strides_of(K), V.data_ptr(),
+                                      _strides_of(V), head_group.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
+                                      None if key_valid is None else key_valid.data_ptr(), out.data_ptr(), ldo, ws.data_ptr(),
+                                      ws.numel(), _stream_of(Q, K, V, head_group, pattern_id, key_valid, out, ws)), "sf_cross_gqa_forward")
     return out
 
 
@@ -731,11 +745,13 @@ _SF_OF = {torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16}
 
 def _rows_of(x: torch.Tensor, what: str):
     """(rows, row stride) of a tensor whose leading dimensions are one run of equally spaced rows."""
-    assert x.dim() >= 1 and (x.shape[-1] <= 1 or x.stride(-1) == 1), f"{what}: the last dimension has to be contiguous"
-    if x.dim() <= 2:
-        return (x.shape[0], x.stride(0)) if x.dim() == 2 else (1, x.shape[-1])
+    n = x.shape[-1]
+    assert x.dim() >= 1 and (n <= 1 or x.stride(-1) == 1), f"{what}: the last dimension has to be contiguous"
+    if x.dim() == 2:
+        assert x.shape[0] <= 1 or x.stride(0) >= n, f"{what}: rows must not overlap"
+        return x.shape[0], x.stride(0) if x.shape[0] > 1 else n
     assert x.is_contiguous(), f"{what}: more than two dimensions have to be contiguous"
-    return x.numel() // max(x.shape[-1], 1), x.shape[-1]
+    return x.numel() // max(n, 1), n
 
 
 def quantize_i8_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
@@ -743,6 +759,7 @@ def quantize_i8_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scal
     more dimensions.  Returns (codes, scale)."""
     rows, ldx = _rows_of(x, "x")
     n = x.shape[-1]
+    assert x.dtype in _SF_OF, x.dtype
     if codes is None:
         codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
     if scale is None:
@@ -750,8 +767,8 @@ def quantize_i8_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scal
     crows, ldc = _rows_of(codes, "codes")
     assert codes.dtype == torch.int8 and codes.shape[-1] == n and crows == rows
     assert scale.dtype == torch.float32 and scale.is_contiguous() and scale.numel() == rows
-    _check(lib().sf_quantize_i8_rows(x.data_ptr(), _SF_OF[x.dtype], rows, n, max(ldx, n), codes.data_ptr(), max(ldc, n), scale.data_ptr(),
-                                     _stream_of(x)), "sf_quantize_i8_rows")
+    _check(lib().sf_quantize_i8_rows(x.data_ptr(), _SF_OF[x.dtype], rows, n, ldx, codes.data_ptr(), ldc, scale.data_ptr(),
+                                     _stream_of(x, codes, scale)), "sf_quantize_i8_rows")
     return codes, scale
 
 
@@ -784,7 +801,7 @@ def linear_i8_forward(lin: LinearI8, X: torch.Tensor, act: int = SF_ACT_NONE, re
     """X [..., K] in fp32 or this build's 16-bit type -> [..., N]; rows are quantised as they come."""
     rows, ldx = _rows_of(X, "X")
     N, K, dt = lin.N, lin.K, X.dtype
-    assert X.shape[-1] == K and (lin.bias is None or lin.bias.dtype == dt)
+    assert X.shape[-1] == K and dt in _SF_OF and (lin.bias is None or lin.bias.dtype == dt)
     if out is None:
         out = torch.empty(X.shape[:-1] + (N,), dtype=dt, device=X.device)
     orows, ldy = _rows_of(out, "out")
@@ -796,8 +813,8 @@ def linear_i8_forward(lin: LinearI8, X: torch.Tensor, act: int = SF_ACT_NONE, re
         r = residual.data_ptr()
     if ws is None:
         ws = workspace(linear_i8_workspace_bytes(max(rows, 1), K), X.device)
-    _check(lib().sf_linear_i8_forward(lin.ref, _SF_OF[dt], rows, X.data_ptr(), max(ldx, K), act, r, max(ldr, N), out.data_ptr(), max(ldy, N),
-                                      ws.data_ptr(), ws.numel(), _stream_of(X)), "sf_linear_i8_forward")
+    _check(lib().sf_linear_i8_forward(lin.ref, _SF_OF[dt], rows, X.data_ptr(), ldx, act, r, ldr, out.data_ptr(), ldy,
+                                      ws.data_ptr(), ws.numel(), _stream_of(X, lin.codes, residual, out, ws)), "sf_linear_i8_forward")
     return out
 
 
@@ -846,7 +863,8 @@ def compact_ffn_i8(desc: SfDesc, layer: int, dense8: Dict[str, torch.Tensor], ma
                                                   ln2_b=dense8.get("ln2_b"), with_b1=b1 is not None, device=dense8["W1"].device)
     assert cf.k_ffn == int(k_ffn)
     ds = SfDenseFfnI8(*[_ptr(t) for t in (dense8["W1"], dense8["W2"], dense8["s1"], b1)])
-    _check(lib().sf_compact_ffn_i8(C.byref(desc), int(layer), C.byref(ds), _ptr(masks["ffn_idx"]), cf.ref, _stream()), "sf_compact_ffn_i8")
+    _check(lib().sf_compact_ffn_i8(C.byref(desc), int(layer), C.byref(ds), _ptr(masks["ffn_idx"]), cf.ref, _stream_of(*[dense8[n] for n in ("W1", "W2", "s1")], b1, masks["ffn_idx"], cf.W1q)),
+           "sf_compact_ffn_i8")
     return cf
 
 
@@ -866,7 +884,7 @@ def pruned_ffn_i8_forward(desc: SfDesc, ffn: CompactFfnI8, X: torch.Tensor, patt
         ws = workspace(pruned_ffn_i8_workspace_bytes(desc, ffn.k_ffn), X.device)
     _check(lib().sf_pruned_ffn_i8_forward(C.byref(desc), ffn.ref, X.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
                                           pre_ln, add_residual, Y.data_ptr(), ws.data_ptr(), ws.numel(),
-                                          _stream_of(X)), "sf_pruned_ffn_i8_forward")
+                                          _stream_of(X, ffn.W1q, pattern_id, Y, ws)), "sf_pruned_ffn_i8_forward")
     return Y
 
 
@@ -964,7 +982,7 @@ def moe_ffn_few_forward(desc: SfDesc, moe: CompactMoe, X: torch.Tensor, pattern_
         ws = workspace(moe_ffn_few_workspace_bytes(desc, moe), dev)
     _check(lib().sf_moe_ffn_few_forward(C.byref(desc), C.byref(moe.struct), X.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
                                         pre_ln, add_residual, fr, Y.data_ptr(), *[None if t is None else t.data_ptr() for t in (route, weight, logit)],
-                                        ws.data_ptr(), ws.numel(), _stream_of(X)), "sf_moe_ffn_few_forward")
+                                        ws.data_ptr(), ws.numel(), _stream_of(X, moe.W1, pattern_id, forced_route, Y, ws)), "sf_moe_ffn_few_forward")
     return (Y, route, weight, logit) if want_route else Y
 
 

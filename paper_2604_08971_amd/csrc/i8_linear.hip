@@ -244,6 +244,7 @@ extern "C" int32_t sf_linear_i8_forward(const sf_linear_i8 *lin, int32_t dtype, 
     if (rows == 0) return SF_OK;
     if (!lin->W || !lin->s || !X || !Y) return fail(SF_ERR_INVALID_ARG, "linear_i8: NULL argument");
     if (X == Y) return fail(SF_ERR_INVALID_ARG, "linear_i8: Y may not alias X");
+    if (R == Y && ldr != ldy) return fail(SF_ERR_INVALID_ARG, "linear_i8: R is Y with rows of another stride");
     const int es = dtype == SF_F32 ? 4 : 2;
     if (((uintptr_t)lin->W & 15) || ((uintptr_t)lin->s & 3) || (((uintptr_t)X | (uintptr_t)Y | (uintptr_t)R | (uintptr_t)lin->bias) % es))
         return fail(SF_ERR_INVALID_ARG, "linear_i8: W aligned to 16 bytes, the others to their elements required");

@@ -655,8 +655,8 @@ extern "C" int32_t sf_moe_ffn_few_forward(const sf_desc *desc, const sf_moe_comp
     if (X == Y) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: Y may not alias X");
     if (!m->Wr || !m->W1 || !m->W2T || (pre_ln && (!m->ln_g || !m->ln_b))) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: NULL parameter pointer");
     if (D.P > 1 && !pattern_id) return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: pattern_id required when P > 1");
-    if (((uintptr_t)X | (uintptr_t)Y | (uintptr_t)m->Wr | (uintptr_t)m->W1 | (uintptr_t)m->W2T) & 15)
-        return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: X, Y, Wr, W1 and W2T must be 16-byte aligned");
+    if (((uintptr_t)X | (uintptr_t)Y | (uintptr_t)m->Wr | (uintptr_t)m->W1 | (uintptr_t)m->W2T | (pre_ln ? (uintptr_t)m->ln_g | (uintptr_t)m->ln_b : 0)) & 15)
+        return fail(SF_ERR_INVALID_ARG, "moe_ffn_few: X, Y, Wr, W1, W2T, ln_g and ln_b must be 16-byte aligned");
     const FewWs w = few_ws(D, *m, workspace);
     if (!workspace || workspace_bytes < w.bytes || ((uintptr_t)workspace & 255))
         return fail(SF_ERR_WORKSPACE, "moe_ffn_few: workspace of %zu bytes (256-byte aligned) required, got %zu", w.bytes, workspace_bytes);
