@@ -276,17 +276,15 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _stream_of(*tensors: Optional[torch.Tensor]) -> int:
+def _stream_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
     """The current stream, for a call on these tensors: all of them have to be on the current device, where the launches go."""
-    device = None
-    for t in tensors:
-        if t is None:
-            continue
-        at = t.get_device()
-        if at < 0 or at != (torch.cuda.current_device() if device is None else device):
-            raise SentryFuseError(f"a tensor on {t.device}, which is not the current device")
-        device = at
-    return torch.cuda.current_stream().cuda_stream
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise SentryFuseError(f"tensors on {first.device} and on {t.device}")
+    if device < 0 or device != torch.cuda.current_device():
+        raise SentryFuseError(f"tensors on {first.device}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def torch_dtype(dtype: int):
@@ -588,8 +586,9 @@ def sparse_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.
 
 def _strides_of(t: torch.Tensor) -> SfStrides:
     """As _strides4, with 0 for a dimension of one element, whose stride says nothing."""
-    assert t.dim() == 4 and t.stride(3) == 1
-    return SfStrides(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+    (nb, nh, nl, _), (b, h, l, e) = t.shape, t.stride()
+    assert e == 1
+    return SfStrides(b if nb > 1 else 0, h if nh > 1 else 0, l if nl > 1 else 0)
 
 
 def cross_gqa_workspace_bytes(desc: SfDesc, Lk: int, nH: int, nG: int) -> int:
@@ -602,17 +601,21 @@ def cross_gqa_forward(desc: SfDesc, Q: torch.Tensor, K: torch.Tensor, V: torch.T
     """Q [B,nH,Lq,dh] over K, V [B,nG,Lk,dh] (last dimension contiguous, any other strides), desc with L = Lq;
     head_group [n_maps,nH] int32, key_valid [B,Lk] u8.  Returns O [B,Lq,nH*dh] (out: row stride any, the same over all samples)."""
     B, nH, Lq, dh = Q.shape
-    nG, Lk, dt = K.shape[1], K.shape[2], Q.dtype
-    assert (desc.B, desc.L, desc.dh) == (B, Lq, dh) and dt == torch_dtype(desc.dtype) == K.dtype == V.dtype
-    assert K.shape == V.shape and K.shape[0] == B and K.shape[3] == dh
+    kv, dt = K.shape, Q.dtype
+    Bk, nG, Lk, dk = kv
+    assert desc.B == B == Bk and desc.L == Lq and desc.dh == dh == dk and kv == V.shape
+    assert dt == torch_dtype(desc.dtype) == K.dtype == V.dtype
     assert head_group.dtype == torch.int32 and head_group.is_contiguous() and head_group.shape[-1] == nH
     assert pattern_id is None or (pattern_id.dtype == torch.int32 and pattern_id.is_contiguous() and pattern_id.numel() == B)
-    assert key_valid is None or (key_valid.dtype == torch.uint8 and key_valid.is_contiguous() and tuple(key_valid.shape) == (B, Lk))
+    assert key_valid is None or (key_valid.dtype == torch.uint8 and key_valid.is_contiguous() and key_valid.shape == (B, Lk))
+    ldo = nH * dh
     if out is None:
-        out = torch.empty((B, Lq, nH * dh), dtype=dt, device=Q.device)
-    assert out.dtype == dt and tuple(out.shape) == (B, Lq, nH * dh) and out.stride(2) == 1
-    assert B == 1 or Lq == 1 or out.stride(0) == Lq * out.stride(1), "out: rows equally spaced over all samples"
-    ldo = out.stride(1) if Lq > 1 else out.stride(0) if B > 1 else nH * dh
+        out = Q.new_empty((B, Lq, ldo))
+    else:
+        sb, sl, se = out.stride()
+        assert out.dtype == dt and out.shape == (B, Lq, ldo) and se == 1
+        assert B == 1 or Lq == 1 or sb == Lq * sl, "out: rows equally spaced over all samples"
+        ldo = sl if Lq > 1 else sb if B > 1 else ldo
     if ws is None:
         ws = workspace(cross_gqa_workspace_bytes(desc, Lk, nH, nG), Q.device)
     _check(lib().sf_cross_gqa_forward(C.byref(desc), nH, nG, Lk, Q.data_ptr(), _strides_of(Q), K.data_ptr(), _strides_of(K), V.data_ptr(),
@@ -745,12 +748,14 @@ _SF_OF = {torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16}
 
 def _rows_of(x: torch.Tensor, what: str):
     """(rows, row stride) of a tensor whose leading dimensions are one run of equally spaced rows."""
-    n = x.shape[-1]
-    assert x.dim() >= 1 and (n <= 1 or x.stride(-1) == 1), f"{what}: the last dimension has to be contiguous"
-    if x.dim() == 2:
-        assert x.shape[0] <= 1 or x.stride(0) >= n, f"{what}: rows must not overlap"
-        return x.shape[0], x.stride(0) if x.shape[0] > 1 else n
-    assert x.is_contiguous(), f"{what}: more than two dimensions have to be contiguous"
+    shape = x.shape
+    n = shape[-1]
+    if len(shape) == 2:
+        rows, (ld, e) = shape[0], x.stride()
+        assert n <= 1 or e == 1, f"{what}: the last dimension has to be contiguous"
+        assert rows <= 1 or ld >= n, f"{what}: rows must not overlap"
+        return rows, ld if rows > 1 else n
+    assert x.is_contiguous(), f"{what}: other than two dimensions have to be contiguous"
     return x.numel() // max(n, 1), n
 
 
@@ -803,9 +808,10 @@ def linear_i8_forward(lin: LinearI8, X: torch.Tensor, act: int = SF_ACT_NONE, re
     N, K, dt = lin.N, lin.K, X.dtype
     assert X.shape[-1] == K and dt in _SF_OF and (lin.bias is None or lin.bias.dtype == dt)
     if out is None:
-        out = torch.empty(X.shape[:-1] + (N,), dtype=dt, device=X.device)
-    orows, ldy = _rows_of(out, "out")
-    assert out.dtype == dt and out.shape[-1] == N and orows == rows
+        out, ldy = X.new_empty(X.shape[:-1] + (N,)), N
+    else:
+        orows, ldy = _rows_of(out, "out")
+        assert out.dtype == dt and out.shape[-1] == N and orows == rows
     r, ldr = None, N
     if residual is not None:
         rrows, ldr = _rows_of(residual, "residual")
@@ -969,17 +975,16 @@ def moe_ffn_few_forward(desc: SfDesc, moe: CompactMoe, X: torch.Tensor, pattern_
     assert pattern_id is None or (pattern_id.dtype == torch.int32 and pattern_id.is_contiguous() and pattern_id.numel() == desc.B)
     Y = torch.empty_like(X) if out is None else out
     assert Y.is_contiguous() and Y.dtype == X.dtype and Y.numel() == X.numel()
-    dev, route, weight, logit, fr = X.device, None, None, None, None
+    route = weight = logit = fr = None
     if want_route:
-        route = torch.empty((rows, moe.top_k), dtype=torch.int32, device=dev)
-        weight = torch.empty((rows, moe.top_k), dtype=torch.float32, device=dev)
-        logit = torch.empty((rows, moe.E), dtype=torch.float32, device=dev)
+        route = X.new_empty((rows, moe.top_k), dtype=torch.int32)
+        weight, logit = X.new_empty((rows, moe.top_k), dtype=torch.float32), X.new_empty((rows, moe.E), dtype=torch.float32)
     if forced_route is not None:
         assert forced_route.dtype == torch.int32 and forced_route.is_contiguous()
         assert tuple(forced_route.shape) == (rows, moe.top_k)
         fr = forced_route.data_ptr()
     if ws is None:
-        ws = workspace(moe_ffn_few_workspace_bytes(desc, moe), dev)
+        ws = workspace(moe_ffn_few_workspace_bytes(desc, moe), X.device)
     _check(lib().sf_moe_ffn_few_forward(C.byref(desc), C.byref(moe.struct), X.data_ptr(), None if pattern_id is None else pattern_id.data_ptr(),
                                         pre_ln, add_residual, fr, Y.data_ptr(), *[None if t is None else t.data_ptr() for t in (route, weight, logit)],
                                         ws.data_ptr(), ws.numel(), _stream_of(X, moe.W1, pattern_id, forced_route, Y, ws)), "sf_moe_ffn_few_forward")
