@@ -5,6 +5,11 @@
 
 namespace sf {
 
+__device__ __forceinline__ uint32_t pack4_i8(int a, int b, int c, int d)
+{
+    return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)d << 24);
+}
+
 // One row's quantiser.  code = rne(127 x / a) with a the row's largest magnitude, scale = a / 127; a = 0: codes and scale 0; an infinity or
 // NaN in the row: codes 0 and scale NaN, so that every product with the row is NaN.
 struct RowCode {
@@ -18,6 +23,26 @@ struct RowCode {
         r = fine ? 127.0f / amax : 0.f;
         if (!fine) pre = 0.f;
         scale = amax_bits < 0x7f800000u ? a / 127.0f : __uint_as_float(0x7fc00000u);
+    }
+    // Eight codes: a rounded quotient that stays away from the borders is the code, and where one of the eight does not, operator() decides all
+    __device__ __forceinline__ uint2 eight(const float *x) const
+    {
+        float c[8], off = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float t = x[e] * pre * r;
+            c[e] = __builtin_rintf(t);
+            off = fmaxf(off, fabsf(t - c[e]));
+        }
+        int k[8];
+        if (off < 0.5f - 2e-5f && r != 0.f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[e] = (int)c[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[e] = (*this)(x[e]);
+        }
+        return make_uint2(pack4_i8(k[0], k[1], k[2], k[3]), pack4_i8(k[4], k[5], k[6], k[7]));
     }
     // x r differs from 127 x / a by less than 1.6e-5 (two roundings of values up to 127): only there a border between two codes is decided in
     // 64 bits, where 254 x and (2 k + 1) a are exact
@@ -35,20 +60,38 @@ struct RowCode {
     }
 };
 
-__device__ __forceinline__ uint32_t pack4_i8(int a, int b, int c, int d)
-{
-    return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)d << 24);
-}
-
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Largest of the lanes of a wave, in each of them
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t x)
+// As pair_sum, for the larger one
+template <int O>
+__device__ __forceinline__ uint32_t pair_max(uint32_t x)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) { const uint32_t y = (uint32_t)__shfl_xor((int)x, o); x = x > y ? x : y; }
-    return x;
+    uint32_t y, z = x;
+    if constexpr (O == 32 || O == 16) {
+        const auto r = O == 32 ? __builtin_amdgcn_permlane32_swap(x, x, false, false) : __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        y = r[0]; z = r[1];
+    } else {
+        constexpr int ctrl = O == 8 ? 0x128 : O == 4 ? 0x124 : O == 2 ? 0x4e : 0xb1;
+        y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, false);
+    }
+    return y > z ? y : z;
 }
+// Largest and sum of each LANES lanes of a wave (16, 32, 64), in each of them
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x)
+{
+    if constexpr (LANES > 32) x = pair_max<32>(x);
+    if constexpr (LANES > 16) x = pair_max<16>(x);
+    return pair_max<1>(pair_max<2>(pair_max<4>(pair_max<8>(x))));
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+    if constexpr (LANES > 32) x = pair_sum<32>(x);
+    if constexpr (LANES > 16) x = pair_sum<16>(x);
+    return pair_sum<1>(pair_sum<2>(pair_sum<4>(pair_sum<8>(x))));
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) { return lanes_max<64>(x); }
 
 // p[n .. n + 3], zeros from N on
 __device__ __forceinline__ f32x4 four(const float *p, int n, int N)

@@ -256,7 +256,7 @@ __global__ __launch_bounds__(WM *WN * 64) void gemm_i8_kernel(GemmI8 a, int tile
 
 // Many rows and features: 256 x 256 values a workgroup, 128 x 128 a wave, one wave per SIMD.  A wave then reads eight fragments for sixteen products
 // and the LDS keeps ahead of the matrix cores (1536 of 2048 clocks per stage, with its writes; tiles of 128 x 128 need 1536 of 1024 and took 181 us for
-// 65 536 x 768 with K 2176).  Stages of 128 bytes of K - whole lines: with stages of 64 or 32 bytes the fetches were what took the time, 173 and 228 us.
+// 65 536 x 768 with K 2176, these 146).  Stages of 128 bytes of K - whole lines: with stages of 64 or 32 bytes the fetches were what took the time, 173 and 228 us.
 // Fragments are read one step of 32 bytes ahead, across the stages: the wait for the next one stands before a stage's last step.
 template <int ACT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
@@ -322,8 +322,8 @@ void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
         }
         __builtin_amdgcn_sched_barrier(0);                   // in this order: the reads return while the products run
     };
-    // A fetch holds up its wave's issue for some 100 clocks where others stand before it (all sixteen in a row: 3650 clocks a stage): two of them, then
-    // four products, from j on
+    // A fetch holds up its wave's issue for some 100 clocks where others stand before it (all sixteen in a row: 157 us for K 2176): one or two, then four
+    // products
     auto multiply = [&](int k, int kt, int slot, int from, int to) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -444,7 +444,8 @@ void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
 // three blocks are 288 of its 512 registers), and every 32 rows pass by it once, through LDS.  A tile kernel reads a row and a feature fragment
 // from LDS for every two or four products; here a row fragment serves TF of them and the features none.  The values of one step are finished (scales,
 // activation, codes) between the products of the next, into whose accumulators they do not go.  A workgroup owns a group of features and a run of
-// rows; where the run comes to a sample of another pattern the weights are fetched again.
+// rows; where the run comes to a sample of another pattern the weights are fetched again.  65 536 rows, K 768, 2176 features: largest values 114 us, codes
+// 124 (128 x 128 tiles 160 and 190).
 // Waiting: a wave's memory operations complete in order as far as vmcnt tells, and it issues the same number each step: F fetches into LDS and E
 // stores (out of range where there is nothing to store).  The last fetch of step s may be the last operation of the turn that issues it; NS - 2 turns
 // follow before it is waited for.
@@ -671,15 +672,16 @@ int32_t launch_act(const GemmI8 &a, hipStream_t st)
     return fail(SF_ERR_UNSUPPORTED, "gemm_i8: this mode takes an activation");
 }
 
-// Tiles: 256 x 256 where whole rounds of one per compute unit hold at least two thirds of values (and for 16-bit values alone), 128 x 128 where they give every
-// compute unit one, 64 x 64 or 32 x 64 with more stages ahead where they do not
+// Tiles: 256 x 256 (for 16-bit values alone) where K is long and whole rounds of one per compute unit are at least 7/8 full: a workgroup's start and end
+// have nothing beside them.  65 536 x 512, 256 x 256 against 128 x 128: K 512 34 and 31 us, K 1024 46 and 45 (2048 features: 181 and 184), K 2048 76
+// and 100; a round 3/4 full, K 2048: 82 and 74.  128 x 128 where they give every compute unit one, 64 x 64 or 32 x 64 with more stages ahead where they do not.
 enum Tile { WIDE, BIG, MIDDLE, SMALL };
 Tile tile_of(const GemmI8 &a, bool values)
 {
     const int64_t samples = a.P > 1 ? a.B : 1, L = a.P > 1 ? a.L : a.B * a.L;
     auto tiles = [&](int m, int n) { return samples * ((L + m - 1) / m) * ((a.N + n - 1) / n); };
     const int64_t rounds = (tiles(256, 256) + 255) / 256;
-    if (values && 3 * samples * L * a.N >= 2 * rounds * 256 * 65536) return WIDE;
+    if (values && a.K >= 1024 && 8 * samples * L * a.N >= 7 * rounds * 256 * 65536) return WIDE;
     return tiles(128, 128) >= 256 ? BIG : tiles(64, 64) >= 256 ? MIDDLE : SMALL;
 }
 

@@ -99,12 +99,7 @@ __global__ __launch_bounds__(256) void i8_few_kernel(FewI8 a)
             for (int e = 0; e < 8; ++e) { const uint32_t u = abs_bits(v[c][e]); m = m > u ? m : u; }
         const RowCode code(wave_max_u32(m));
 #pragma unroll
-        for (int c = 0; c < NCH; ++c) {
-            uint2 o;
-            o.x = pack4_i8(code(v[c][0]), code(v[c][1]), code(v[c][2]), code(v[c][3]));
-            o.y = pack4_i8(code(v[c][4]), code(v[c][5]), code(v[c][6]), code(v[c][7]));
-            *reinterpret_cast<uint2 *>(&xq[r][(lane + c * 64) * 8]) = o;
-        }
+        for (int c = 0; c < NCH; ++c) *reinterpret_cast<uint2 *>(&xq[r][(lane + c * 64) * 8]) = code.eight(v[c]);
         if (lane == 0) xs[r] = code.scale;
     }
     __syncthreads();

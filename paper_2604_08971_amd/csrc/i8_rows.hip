@@ -1,80 +1,87 @@
 // Quantisers of rows to 8-bit integers, one scale per row: alone and behind a LayerNorm.
 //
-// A row is read once and stays in registers (a wave per row, up to 4096 elements), so what bounds it is memory: es bytes read and one
-// written per element.
+// A row is read once and stays in registers (up to 4096 elements), so what bounds it is memory: es bytes read and one written per element.  A
+// wave per row has too little on its way where rows are short: 65 536 rows of 64, 512 and 768 bf16 elements took 27, 29 and 35 us that way, and take 7,
+// 21 and 28 with the rows of a wave's lanes next to each other and four (two) of them at once; behind a LayerNorm 49 and now 45 us for 768.
 #include "i8.hpp"
 
 namespace sf {
 
 namespace {
 
-template <class T, int NCH, bool LN>
+template <class T> struct Raw;
+template <> struct Raw<h16> { typedef h16x8 type; };
+template <> struct Raw<float> { typedef __attribute__((ext_vector_type(8), aligned(16))) float type; };
+
+// LANES lanes a row, NCH times eight elements each, NR rows of a lane with their loads in flight together
+template <class T, int NCH, int LANES, int NR, bool LN>
 __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ X, int64_t ldx, int64_t rows, int n, const h16 *__restrict__ g,
                                                       const h16 *__restrict__ b, float eps, int8_t *__restrict__ codes, int64_t ldc,
                                                       float *__restrict__ scale)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const T *x = X + row * ldx;
-    float v[NCH][8];
-    float sum = 0.f;
+    constexpr int SIDE = 64 / LANES;                         // rows next to each other in a wave
+    const int lane = threadIdx.x & (LANES - 1);
+    const int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (NR * SIDE) + (threadIdx.x & 63) / LANES;
+    typedef typename Raw<T>::type Eight;
+    Eight raw[NR][NCH];
+    h16x8 gm[LN ? NCH : 1], bt[LN ? NCH : 1];
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-        const int at = (lane + c * 64) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] = 0.f;
-        if (at < n) {
-            if constexpr (sizeof(T) == 2) {
-                const h16x8 t = *reinterpret_cast<const h16x8 *>(x + at);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[c][e] = (float)t[e];
-            } else {
-                const f32x4 t0 = *reinterpret_cast<const f32x4 *>(x + at), t1 = *reinterpret_cast<const f32x4 *>(x + at + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { v[c][e] = t0[e]; v[c][4 + e] = t1[e]; }
-            }
-            if constexpr (LN) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[c][e];
-            }
-        }
-    }
-    if constexpr (LN) {
-        const float mean = wave_sum(sum) / n;
-        float q = 0.f;
-#pragma unroll
-        for (int c = 0; c < NCH; ++c)
-            if ((lane + c * 64) * 8 < n) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { v[c][e] -= mean; q = fmaf(v[c][e], v[c][e], q); }
-            }
-        const float inv = 1.0f / sqrtf(wave_sum(q) / n + eps);
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
         for (int c = 0; c < NCH; ++c) {
-            const int at = (lane + c * 64) * 8;
-            if (at >= n) continue;
-            const h16x8 gm = *reinterpret_cast<const h16x8 *>(g + at), bt = *reinterpret_cast<const h16x8 *>(b + at);
+            const int at = (lane + c * LANES) * 8;
+            raw[i][c] = Eight{};
+            if (at < n && row0 + i * SIDE < rows) raw[i][c] = *reinterpret_cast<const Eight *>(X + (row0 + i * SIDE) * ldx + at);
+        }
+    if constexpr (LN) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[c][e] = fmaf(v[c][e] * inv, (float)gm[e], (float)bt[e]);
+        for (int c = 0; c < NCH; ++c) {
+            const int at = (lane + c * LANES) * 8;
+            gm[c] = bt[c] = h16x8{};
+            if (at < n) { gm[c] = *reinterpret_cast<const h16x8 *>(g + at); bt[c] = *reinterpret_cast<const h16x8 *>(b + at); }
         }
     }
-    uint32_t m = 0;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
+    for (int i = 0; i < NR; ++i) {
+        const int64_t row = row0 + i * SIDE;
+        if (row >= rows) break;
+        float v[NCH][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { const uint32_t u = abs_bits(v[c][e]); m = m > u ? m : u; }
-    const RowCode code(wave_max_u32(m));
+        for (int c = 0; c < NCH; ++c)
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-        const int at = (lane + c * 64) * 8;
-        if (at >= n) continue;
-        uint2 o;
-        o.x = pack4_i8(code(v[c][0]), code(v[c][1]), code(v[c][2]), code(v[c][3]));
-        o.y = pack4_i8(code(v[c][4]), code(v[c][5]), code(v[c][6]), code(v[c][7]));
-        *reinterpret_cast<uint2 *>(codes + row * ldc + at) = o;
+            for (int e = 0; e < 8; ++e) v[c][e] = (float)raw[i][c][e];
+        if constexpr (LN) {
+            float sum = 0.f, q = 0.f;
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += v[c][e];
+            const float mean = lanes_sum<LANES>(sum) / n;
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+                if ((lane + c * LANES) * 8 < n) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { v[c][e] -= mean; q = fmaf(v[c][e], v[c][e], q); }
+                }
+            const float inv = 1.0f / sqrtf(lanes_sum<LANES>(q) / n + eps);
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[c][e] = fmaf(v[c][e] * inv, (float)gm[c][e], (float)bt[c][e]);       // zeros behind the row
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { const uint32_t u = abs_bits(v[c][e]); m = m > u ? m : u; }
+        const RowCode code(lanes_max<LANES>(m));
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int at = (lane + c * LANES) * 8;
+            if (at < n) *reinterpret_cast<uint2 *>(codes + row * ldc + at) = code.eight(v[c]);
+        }
+        if (lane == 0) scale[row] = code.scale;
     }
-    if (lane == 0) scale[row] = code.scale;
 }
 
 // Rows of any length, stride and alignment: a workgroup per row, read twice
@@ -108,16 +115,21 @@ void launch_rows(const I8Rows &a, int64_t ldc, bool vec, hipStream_t st)
         hipLaunchKernelGGL(i8_rows_any_kernel<T>, dim3(grid), dim3(256), 0, st, X, a.ldx, a.rows, a.K, a.codes, ldc, a.scale);
         return;
     }
-    const dim3 grid((unsigned)((a.rows + 3) / 4));
-#define SF_I8_ROWS(NCH, LN)                                                                                                      \
-    hipLaunchKernelGGL((i8_rows_kernel<T, NCH, LN>), grid, dim3(256), 0, st, X, a.ldx, a.rows, a.K, (const h16 *)a.ln_g, (const h16 *)a.ln_b, \
-                       a.eps, a.codes, ldc, a.scale)
+#define SF_I8_ROWS(NCH, LANES, NR, LN)                                                                                           \
+    hipLaunchKernelGGL((i8_rows_kernel<T, NCH, LANES, NR, LN>), dim3((unsigned)((a.rows + 256 / LANES * NR - 1) / (256 / LANES * NR))),   \
+                       dim3(256), 0, st, X, a.ldx, a.rows, a.K, (const h16 *)a.ln_g, (const h16 *)a.ln_b, a.eps, a.codes, ldc, a.scale)
+    // a wave for every row until the chip holds no more of them (8192); from there on more of a row's bytes on their way in each
+    const bool many = a.rows >= 16384;
 #define SF_I8_ROWS_N(LN)                                                                                                         \
     do {                                                                                                                         \
-        if (a.K <= 512) SF_I8_ROWS(1, LN);                                                                                       \
-        else if (a.K <= 1024) SF_I8_ROWS(2, LN);                                                                                 \
-        else if (a.K <= 2048) SF_I8_ROWS(4, LN);                                                                                 \
-        else SF_I8_ROWS(8, LN);                                                                                                  \
+        if (many && a.K <= 128) SF_I8_ROWS(1, 16, 4, LN);                                                                        \
+        else if (many && a.K <= 256) SF_I8_ROWS(1, 32, 4, LN);                                                                   \
+        else if (many && a.K <= 512) SF_I8_ROWS(1, 64, 4, LN);                                                                   \
+        else if (many && a.K <= 1024) SF_I8_ROWS(2, 64, 2, LN);                                                                  \
+        else if (a.K <= 512) SF_I8_ROWS(1, 64, 1, LN);                                                                           \
+        else if (a.K <= 1024) SF_I8_ROWS(2, 64, 1, LN);                                                                          \
+        else if (a.K <= 2048) SF_I8_ROWS(4, 64, 1, LN);                                                                          \
+        else SF_I8_ROWS(8, 64, 1, LN);                                                                                           \
     } while (0)
     if constexpr (sizeof(T) == 2) {
         if (a.ln_g) { SF_I8_ROWS_N(true); return; }
