@@ -445,7 +445,7 @@ void gemm_i8_wide_kernel(GemmI8 a, int tiles_n, int tiles_l, int in_line)
 // from LDS for every two or four products; here a row fragment serves TF of them and the features none.  The values of one step are finished (scales,
 // activation, codes) between the products of the next, into whose accumulators they do not go.  A workgroup owns a group of features and a run of
 // rows; where the run comes to a sample of another pattern the weights are fetched again.  65 536 rows, K 768, 2176 features: largest values 114 us, codes
-// 124 (128 x 128 tiles 160 and 190).
+// 124 (tiles of 128 x 128: 145 and 230).
 // Waiting: a wave's memory operations complete in order as far as vmcnt tells, and it issues the same number each step: F fetches into LDS and E
 // stores (out of range where there is nothing to store).  The last fetch of step s may be the last operation of the turn that issues it; NS - 2 turns
 // follow before it is waited for.
