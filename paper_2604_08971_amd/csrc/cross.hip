@@ -105,12 +105,13 @@ __device__ __forceinline__ int tiles_of(KeyTiles<KT, MASK> &t, const uint8_t *va
 }
 
 // ------------------------------------------------------------------------------------------------- 16-bit models
-// WQ waves along the rows (QB blocks of 32 each), WK along the keys
-template <int DH, int WQ, int WK, int QB, bool MASK>
-__global__ __launch_bounds__(WQ *WK * 64, 2) void cross_kernel(CrossArgs a)
+// WQ waves along the rows (QB blocks of 32 each), WK along the keys.  Two blocks a wave read a fragment of K and V once for both: 16 samples of 2048
+// queries and keys, twelve heads of 64 gained 1 % (239 to 236 us), 64 samples of 512 lost 13 % (49 to 56) - one block it is.
+template <int DH, int WQ, int WK, bool MASK>
+__global__ __launch_bounds__(WQ *WK * 64, DH == 128 && WK == 4 ? 1 : 2) void cross_kernel(CrossArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int KT = WK == 4 ? 32 : 64, RB = DH * 2, CH = DH / 8;       // keys of a tile, bytes and 16-byte chunks of a row
+    constexpr int QB = 1, KT = WK == 4 ? 32 : 64, RB = DH * 2, CH = DH / 8;       // keys of a tile, bytes and 16-byte chunks of a row
     constexpr int TILE = KT * RB, STAGE = WK * 2 * TILE, PIECES = TILE / 1024, ROWS = WQ * QB * 32;
     constexpr int JOIN = WK > 1 ? WK * 32 * (DH + 2) * 4 : 0;
     __shared__ __attribute__((aligned(128))) char lds[2 * STAGE > JOIN ? 2 * STAGE : JOIN];
@@ -569,19 +570,21 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a, int groups
     }
 }
 
-// How a call runs: waves along rows and keys, blocks of rows per wave, key ranges
-struct CrossPlan { int wq, wk, qb, kt, runs, splits, tiles_per_split; size_t part, bytes; };
+// How a call runs: waves along rows and keys, key ranges.
+// Waves along the keys where a group has at most one block of rows, so that none idles (64 samples of ten queries, 1024 keys: 17.7 us, along the rows
+// 18.8; 256 of four, 480 keys: 26.4 and 26.8; eight of eight, 2048 keys: 13.0 and 11.4).  Key ranges of workgroups of their own where these are fewer
+// than the compute units, towards two for each (one query, 4096 keys: 8.7 us, without 22.6; four samples of 128, 4096 keys: 18 and 56).
+struct CrossPlan { int wq, wk, kt, runs, splits, tiles_per_split; size_t part, bytes; };
 CrossPlan cross_plan(const Dims &D, int64_t Lk, int nH, int nG)
 {
     CrossPlan p{};
     const bool half = D.dtype == SF_BF16;
     const int64_t rows = (int64_t)nH * D.L;                   // of all groups of a sample
     const int64_t mean = (rows + nG - 1) / nG;
-    p.wq = 4; p.wk = 1; p.qb = 1;
+    p.wq = 4; p.wk = 1;
     if (mean <= 32) { p.wq = 1; p.wk = 4; }
-    else if (half && D.dh <= 64 && mean >= 256 && rows / 256 * D.B >= 512) p.qb = 2;
     p.kt = half && p.wk == 1 ? 64 : 32;
-    const int own = p.wq * p.qb * 32;
+    const int own = p.wq * 32;
     p.runs = (int)(rows / own) + nG;                          // at least the runs of all groups, whatever the heads' map
     const int64_t blocks = (int64_t)D.B * ((rows + own - 1) / own > nG ? (rows + own - 1) / own : nG);
     const int64_t tiles = (Lk + p.kt - 1) / p.kt;
@@ -611,21 +614,18 @@ int32_t check_cross(const Dims &D, int32_t Lk, int32_t nH, int32_t nG)
     return SF_OK;
 }
 
-template <int DH, int WQ, int WK, int QB>
+template <int DH, int WQ, int WK>
 void launch16(const CrossArgs &a, const CrossPlan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)p.runs, (unsigned)a.B, (unsigned)p.splits), block(WQ * WK * 64);
-    if (a.key_valid) hipLaunchKernelGGL((cross_kernel<DH, WQ, WK, QB, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((cross_kernel<DH, WQ, WK, QB, false>), grid, block, 0, st, a);
+    if (a.key_valid) hipLaunchKernelGGL((cross_kernel<DH, WQ, WK, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((cross_kernel<DH, WQ, WK, false>), grid, block, 0, st, a);
 }
 template <int DH>
 void launch_dh(const CrossArgs &a, const CrossPlan &p, hipStream_t st)
 {
-    if (p.wk == 4) launch16<DH, 1, 4, 1>(a, p, st);
-    else if constexpr (DH <= 64) {
-        if (p.qb == 2) launch16<DH, 4, 1, 2>(a, p, st);
-        else launch16<DH, 4, 1, 1>(a, p, st);
-    } else launch16<DH, 4, 1, 1>(a, p, st);
+    if (p.wk == 4) launch16<DH, 1, 4>(a, p, st);
+    else launch16<DH, 4, 1>(a, p, st);
 }
 template <int WQ, int WK, bool MASK>
 int32_t launch32(const CrossArgs &a, const CrossPlan &p, hipStream_t st)

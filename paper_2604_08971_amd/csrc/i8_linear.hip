@@ -21,7 +21,8 @@ __device__ __forceinline__ int row16_sum(int x)
 
 // Quantiser and product of up to R rows in one launch (blockIdx.y: sample).  What bounds it is the weights, read once, and one memory round
 // trip each for them, the rows and the reduction.  Every workgroup quantises the rows for itself, into LDS, while its first weights are on
-// their way; 16 lanes then share a feature, 16 bytes of K each at a time (v_dot4), and join their sums at the end.
+// their way; 16 lanes then share a feature, 16 bytes of K each at a time (v_dot4), and join their sums at the end.  Up to eight rows of up to 4096:
+// one row, 512 x 512 3.1 us (quantiser and product in launches of their own 5.7), eight rows 4.8 (6.3), eight of 4096 x 768 15.7 (17.0).
 struct FewI8 {
     const void *X; int64_t ldx; int64_t x_bstride; int rows, K;          // rows of a sample
     const void *ln_g, *ln_b; float eps;

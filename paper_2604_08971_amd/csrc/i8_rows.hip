@@ -118,8 +118,8 @@ void launch_rows(const I8Rows &a, int64_t ldc, bool vec, hipStream_t st)
 #define SF_I8_ROWS(NCH, LANES, NR, LN)                                                                                           \
     hipLaunchKernelGGL((i8_rows_kernel<T, NCH, LANES, NR, LN>), dim3((unsigned)((a.rows + 256 / LANES * NR - 1) / (256 / LANES * NR))),   \
                        dim3(256), 0, st, X, a.ldx, a.rows, a.K, (const h16 *)a.ln_g, (const h16 *)a.ln_b, a.eps, a.codes, ldc, a.scale)
-    // a wave for every row until the chip holds no more of them (8192); from there on more of a row's bytes on their way in each
-    const bool many = a.rows >= 16384;
+    // a wave for every row until the chip holds no more of them (8192); well above that, more rows on their way in each
+    const bool many = a.rows >= (a.K <= 512 ? 16384 : 32768);
 #define SF_I8_ROWS_N(LN)                                                                                                         \
     do {                                                                                                                         \
         if (many && a.K <= 128) SF_I8_ROWS(1, 16, 4, LN);                                                                        \
